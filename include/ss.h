@@ -21,6 +21,12 @@
  *   ss_process_logits  materialised processed logits and final probabilities
  *   ss_logprobs        top-k log-probabilities under the full-row distribution
  *                      (indicator bit 0x400, Section 3.5)
+ * and the operators at the two ends of the vocabulary, which make the logits
+ * that these read and take up the tokens that they give:
+ *   ss_head_w4         logits of hidden states under a 4-bit vocabulary table
+ *   ss_embed, ss_embed_w4   rows of the vocabulary table by token
+ *   ss_embed_grad      the gradient of such a lookup, by sorted tokens
+ *   ss_quant_w4        the 4-bit form of a vocabulary table
  *
  * Conventions (all functions):
  *   - Every array argument is a DEVICE pointer owned by the caller, except
@@ -100,6 +106,8 @@ typedef int32_t ss_status;
 #define SS_MAX_K 4096      /* k_max upper bound                                    */
 #define SS_MAX_L 16        /* draft length upper bound                             */
 #define SS_MAX_V (1 << 20) /* vocabulary upper bound                               */
+#define SS_MAX_T (1 << 20) /* rows of a head, lookup or gradient call              */
+#define SS_MAX_H (1 << 16) /* columns of a vocabulary table                        */
 
 /*
  * Per-request parameters (host struct of device pointers), read at call time.
@@ -324,6 +332,106 @@ ss_status ss_logprobs(const void *logits, int dtype, int64_t ld, const ss_params
 ss_status ss_sample_noalloc(const void *logits, int dtype, int64_t ld, const ss_params *p, int k_max,
                             int32_t *out_token, float *out_logprob, int32_t *out_idx, float *out_prob,
                             int k_out, int32_t *flags, void *stream);
+
+/*
+ * A vocabulary table in 4 bits (host struct of device pointers, read at call
+ * time): V rows of H columns, a scale for each `group` columns.
+ *   fmt     SS_W4_INT: integers -7..7 with a bfloat16 scale for each 32, 64 or 128
+ *           columns.  SS_W4_MX: E2M1 numbers (0, .5, 1, 1.5, 2, 3, 4, 6 and their
+ *           negatives) with a scale 2^(x - 127), x one byte (255: NaN), for
+ *           each 32 columns.  H is a multiple of `group`.
+ *   codes   ceil(H / 128) blocks of 64 bytes a row.  Dword 4 g + j of a block (g, j
+ *           = 0..3, little-endian) holds its columns 32 j + 8 g + e, e = 0..7.
+ *           SS_W4_MX: column e in bits 4 e .. 4 e + 3.  SS_W4_INT: with bytes
+ *           s0000mmm (sign and magnitude), A those of e = 0..3 and B those of e =
+ *           4..7, lowest byte first: A | rotl32(B, 4).
+ *   scales  ceil(H / 128) * 128 / group a row, in column order.
+ * What stands for columns beyond H in a row's last block takes no part in
+ * any result.  Both pointers are aligned to 16 bytes, rows follow one another.
+ * The value of a column is code * scale.  Group scales of SS_W4_MX below 2^-125
+ * give weights that are subnormal in bfloat16; ss_head_w4 may take those as zero.
+ */
+#define SS_W4_INT 0
+#define SS_W4_MX 1
+typedef struct ss_w4 {
+  int32_t V;
+  int32_t H;
+  int32_t fmt;
+  int32_t group;
+  const void *codes;
+  const void *scales;
+} ss_w4;
+
+/* Bytes of a table's two arrays (host only, pure; the pointers are not looked
+ * at).  0 for sizes or formats that are not offered. */
+size_t ss_w4_codes_bytes(const ss_w4 *t);
+size_t ss_w4_scales_bytes(const ss_w4 *t);
+
+/*
+ * The 4-bit form of a table, for serving what was trained: writes the codes and
+ * scales that `t` points to, for each group of a row from its largest
+ * magnitude a:
+ *   SS_W4_INT  s = a / 7 rounded to float32 and then to bfloat16, code = w / s rounded
+ *              to the nearest integer (ties to even) of -7..7; s = 0 gives codes 0.
+ *   SS_W4_MX   2^e with e = floor(log2 a) - 2, not below -127; code = w / 2^e
+ *              rounded to the nearest E2M1 number (ties to the even code), at most 6.
+ * Quotients are rounded once, as if exact.  A group that holds a NaN or an
+ * infinity gets a NaN scale and codes 0.  Columns beyond H are filled with zeros.
+ *   w       [V, ld] of `dtype`, ld >= H.
+ *   values  NULL, or [V, ld_values] of `values_dtype`: the numbers that the codes stand for
+ *           (code * scale, rounded once), as training against the quantised table needs.
+ */
+ss_status ss_quant_w4(const void *w, int dtype, int64_t ld, const ss_w4 *t, void *values, int values_dtype,
+                      int64_t ld_values, void *stream);
+
+/* Workspace bytes of ss_head_w4 (host only, pure).  0 for invalid sizes. */
+size_t ss_head_w4_bytes(int T, int H, int dtype);
+
+/*
+ * Logits of hidden states under a 4-bit table:
+ *     logits[t, v] = sum_k h[t, k] * W[v, k]
+ * with products exact and sums in float32 (float32 hidden states are taken whole, as three
+ * bfloat16 parts), rounded once to `out_dtype`.  The sampler's entry points read the result.
+ * A row does not depend on the values of the other rows.
+ *   h       [T, ld_h] of `dtype` (SS_F32 or SS_BF16), 0 <= T <= SS_MAX_T, ld_h >= t->H.
+ *   logits  [T, ld] of `out_dtype`, ld >= t->V; columns beyond V are left as they were.
+ *   ws      ss_head_w4_bytes(T, t->H, dtype) bytes, 16-byte aligned.
+ * An infinite or NaN hidden state makes its whole row non-finite or NaN; other rows are not touched.
+ */
+ss_status ss_head_w4(const void *h, int dtype, int T, int64_t ld_h, const ss_w4 *t, void *logits, int out_dtype,
+                     int64_t ld, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Rows of a vocabulary table by token: out[t, :] = scale * table[tokens[t], :], in
+ * float32 and rounded once.  A token outside [0, V) (the padding -1 of
+ * ss_verify, the token -1 of an empty row) gives a row of zeros.
+ *   tokens  int32[T], 0 <= T <= SS_MAX_T.
+ *   table   [V, ld] of `dtype`, ld >= H, 1 <= H <= SS_MAX_H; for ss_embed_w4 a 4-bit table.
+ *   out     [T, ld_out] of `out_dtype`, ld_out >= H.
+ */
+ss_status ss_embed(const int32_t *tokens, int T, const void *table, int dtype, int V, int H, int64_t ld, float scale,
+                   void *out, int out_dtype, int64_t ld_out, void *stream);
+ss_status ss_embed_w4(const int32_t *tokens, int T, const ss_w4 *t, float scale, void *out, int out_dtype,
+                      int64_t ld_out, void *stream);
+
+/* Workspace bytes of ss_embed_grad (host only, pure).  0 for invalid sizes. */
+size_t ss_embed_grad_bytes(int T, int V, int H);
+
+/*
+ * The gradient of a lookup with respect to its table:
+ *     dtable[v, :] = scale * sum over t with tokens[t] = v of dout[t, :]
+ * for all V rows (zeros where no token names the row).  With `accumulate`, it
+ * is added to what dtable holds, and rows that no token names are left as they
+ * were.  Tokens outside [0, V) are passed over.  Sums are taken in float32 in an
+ * order that the tokens alone determine, and rounded once to `out_dtype`: the
+ * same call gives the same bits.
+ *   dout    [T, ld] of `dtype`, 0 <= T <= SS_MAX_T, ld >= H.
+ *   dtable  [V, ld_out] of `out_dtype`, ld_out >= H.
+ *   ws      ss_embed_grad_bytes(T, V, H) bytes, 16-byte aligned.
+ */
+ss_status ss_embed_grad(const void *dout, int dtype, int T, int64_t ld, const int32_t *tokens, int V, int H,
+                        float scale, void *dtable, int out_dtype, int64_t ld_out, int accumulate, void *ws,
+                        size_t ws_bytes, void *stream);
 
 const char *ss_status_string(ss_status s);
 

@@ -24,6 +24,7 @@ GREEDY, TOPK, TOPP, MINP, LOGPROBS = 0x040, 0x080, 0x100, 0x200, 0x400
 FLAG_EMPTY, FLAG_FALLBACK, FLAG_OUT_TRUNC, FLAG_KCAP = 1, 2, 4, 8
 OP_TOPK, OP_SAMPLE, OP_VERIFY, OP_PROCESS, OP_LOGPROBS = 0, 1, 2, 3, 4
 F32, BF16 = 0, 1
+W4_INT, W4_MX = 0, 1
 
 _lib = None
 
@@ -43,6 +44,11 @@ class _Params(C.Structure):
         ("bitmask", C.c_void_p), ("bitmask_ld", C.c_int64),
         ("seed", C.c_void_p), ("position", C.c_void_p),
     ]
+
+
+class _W4(C.Structure):
+    _fields_ = [("V", C.c_int32), ("H", C.c_int32), ("fmt", C.c_int32), ("group", C.c_int32),
+                ("codes", C.c_void_p), ("scales", C.c_void_p)]
 
 
 # _Params as bytes: B, V, fourteen pointers, bitmask_ld, seed, position (one pack
@@ -95,6 +101,23 @@ def lib():
             L.ss_logprobs.argtypes = [vp, C.c_int, i64, vp, C.c_int, vp, vp, vp, vp, sz, vp]
         L.ss_process_logits.restype = i32
         L.ss_process_logits.argtypes = [vp, C.c_int, i64, vp, C.c_int, vp, vp, vp, vp, sz, vp]
+        L.ss_w4_codes_bytes.restype = L.ss_w4_scales_bytes.restype = sz
+        L.ss_w4_codes_bytes.argtypes = L.ss_w4_scales_bytes.argtypes = [vp]
+        L.ss_quant_w4.restype = i32
+        L.ss_quant_w4.argtypes = [vp, C.c_int, i64, vp, vp, C.c_int, i64, vp]
+        L.ss_head_w4_bytes.restype = sz
+        L.ss_head_w4_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
+        L.ss_head_w4.restype = i32
+        L.ss_head_w4.argtypes = [vp, C.c_int, C.c_int, i64, vp, vp, C.c_int, i64, vp, sz, vp]
+        L.ss_embed.restype = i32
+        L.ss_embed.argtypes = [vp, C.c_int, vp, C.c_int, C.c_int, C.c_int, i64, C.c_float, vp, C.c_int, i64, vp]
+        L.ss_embed_w4.restype = i32
+        L.ss_embed_w4.argtypes = [vp, C.c_int, vp, C.c_float, vp, C.c_int, i64, vp]
+        L.ss_embed_grad_bytes.restype = sz
+        L.ss_embed_grad_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
+        L.ss_embed_grad.restype = i32
+        L.ss_embed_grad.argtypes = [vp, C.c_int, C.c_int, i64, vp, C.c_int, C.c_int, C.c_float, vp, C.c_int, i64,
+                                    C.c_int, vp, sz, vp]
         L.ss_status_string.restype = C.c_char_p
         L.ss_status_string.argtypes = [i32]
         _lib = L
@@ -431,6 +454,176 @@ def process_logits(logits, params, k_max, out_logits=None, out_probs=None, flags
     _check(lib().ss_process_logits(_ptr(logits), dt, logits.stride(0), p, k_max, _ptr(out_logits),
                                    _ptr(out_probs), _ptr(flags), _ptr(ws), ws.numel(), _stream()))
     return out_logits, out_probs, flags
+
+
+# ---------------------------------------------------------------------------
+# The two ends of the vocabulary: hidden states to logits, tokens to hidden states
+# ---------------------------------------------------------------------------
+def _rows(t, name, rows=None, cols=None, dtype=None, device=None):
+    """Checks a matrix whose rows are evenly strided and whose columns follow one another."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise SSError(f"{name} must be a matrix of rows with unit column stride")
+    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise SSError(f"{name} must be [{rows}, {cols}], got {list(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise SSError(f"{name} must be {dtype}, got {t.dtype}")
+    _here(t, name, device)
+
+
+def _here(t, name, device=None):
+    """Calls go to the current device's current stream: what they read has to be there."""
+    if not t.is_cuda:
+        raise SSError(f"{name} is not on a GPU")
+    if t.device.index != torch.cuda.current_device() or (device is not None and t.device != device):
+        raise SSError(f"{name} is not on the current device")
+
+
+def _ld(t):
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _tokens(tokens):
+    if tokens.dim() != 1 or tokens.dtype != torch.int32 or not tokens.is_contiguous():
+        raise SSError("tokens must be contiguous int32 [T]")
+    _here(tokens, "tokens")
+    return tokens.shape[0]
+
+
+
+class W4:
+    """A vocabulary table in 4 bits (``ss_w4`` in ss.h): codes uint8 [V, 64 ceil(H / 128)] and scales
+    [V, ceil(H / 128) 128 / group], bfloat16 for ``fmt`` "int" (groups of 32, 64 or 128 columns) and
+    uint8 for "mx" (groups of 32)."""
+
+    FMT = {"int": W4_INT, "mx": W4_MX}
+
+    def __init__(self, codes, scales, V, H, fmt="int", group=128):
+        st, nb = W4._sizes(V, H, fmt, group)
+        if codes.dtype != torch.uint8 or not codes.is_contiguous() or codes.shape != (V, 64 * nb):
+            raise SSError(f"codes must be contiguous uint8 [{V}, {64 * nb}]")
+        dt = torch.uint8 if fmt == "mx" else torch.bfloat16
+        if scales.dtype != dt or not scales.is_contiguous() or scales.shape != (V, nb * 128 // group):
+            raise SSError(f"scales must be contiguous {dt} [{V}, {nb * 128 // group}]")
+        if codes.device != scales.device:
+            raise SSError("codes and scales are on different devices")
+        self.V, self.H, self.fmt, self.group = int(V), int(H), fmt, int(group)
+        self.codes, self.scales = codes, scales
+        st.codes, st.scales = codes.data_ptr(), scales.data_ptr()
+        self._struct = st
+        self._ref = C.addressof(st)
+
+    @staticmethod
+    def _sizes(V, H, fmt, group):
+        if fmt not in W4.FMT:
+            raise SSError(f"format {fmt!r} is neither int nor mx")
+        st = _W4(V=int(V), H=int(H), fmt=W4.FMT[fmt], group=int(group))
+        if lib().ss_w4_codes_bytes(C.byref(st)) == 0:
+            raise SSError(f"no {fmt} table of {V} rows, {H} columns and groups of {group}")
+        return st, (int(H) + 127) // 128
+
+    @classmethod
+    def empty(cls, V, H, fmt="int", group=128, device="cuda"):
+        """A table for ``quantize_w4`` to fill."""
+        nb = W4._sizes(V, H, fmt, group)[1]
+        return cls(torch.empty(V, 64 * nb, dtype=torch.uint8, device=device),
+                   torch.empty(V, nb * 128 // group, dtype=torch.uint8 if fmt == "mx" else torch.bfloat16, device=device),
+                   V, H, fmt, group)
+
+
+def quantize_w4(w, table=None, fmt="int", group=128, values=None):
+    """The 4-bit form of w [V, H] (bfloat16 or float32), written to ``table`` (a new one of ``fmt`` and ``group`` if
+    None) and returned; ``values`` [V, H], if given, gets the numbers that the codes stand for."""
+    _rows(w, "w")
+    if table is None:
+        table = W4.empty(w.shape[0], w.shape[1], fmt, group, w.device)
+    if w.shape != (table.V, table.H):
+        raise SSError(f"w must be [{table.V}, {table.H}], got {list(w.shape)}")
+    _here(table.codes, "table")
+    if values is not None:
+        _rows(values, "values", table.V, table.H)
+    _check(lib().ss_quant_w4(_ptr(w), _dtype_code(w), _ld(w), table._ref, _ptr(values),
+                             F32 if values is None else _dtype_code(values), 0 if values is None else _ld(values),
+                             _stream()))
+    return table
+
+
+def head_workspace(h):
+    """A workspace for ``head_w4`` of hidden states h (or any with as many or fewer rows)."""
+    n = int(lib().ss_head_w4_bytes(h.shape[0], h.shape[1], _dtype_code(h)))
+    if n == 0:
+        raise SSError("invalid sizes for workspace")
+    return torch.empty(n, dtype=torch.uint8, device=h.device)
+
+
+def head_w4(h, table, out=None, dtype=None, ws=None):
+    """Logits [T, V] of hidden states h [T, H] under a 4-bit table; ``dtype`` (of a new ``out``): that of h."""
+    _rows(h, "h", cols=table.H)
+    _here(table.codes, "table")
+    T = h.shape[0]
+    if out is None:
+        out = torch.empty(T, table.V, dtype=dtype or h.dtype, device=h.device)
+    else:
+        _rows(out, "out", T, table.V, dtype)
+    if ws is None:
+        ws = head_workspace(h)
+    _here(ws, "ws")
+    _check(lib().ss_head_w4(_ptr(h), _dtype_code(h), T, _ld(h), table._ref, _ptr(out), _dtype_code(out), _ld(out),
+                            _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    return out
+
+
+def embed(tokens, table, scale=1.0, out=None, dtype=None):
+    """scale * table[tokens] for int32 tokens [T] and a table [V, H] (a matrix or a ``W4``); tokens outside
+    [0, V) give rows of zeros.  ``dtype`` (of a new ``out``): the matrix's, bfloat16 for a ``W4``."""
+    T = _tokens(tokens)
+    w4 = isinstance(table, W4)
+    if w4:
+        V, H = table.V, table.H
+        _here(table.codes, "table")
+    else:
+        _rows(table, "table")
+        V, H = table.shape
+    if out is None:
+        out = torch.empty(T, H, dtype=dtype or (torch.bfloat16 if w4 else table.dtype), device=tokens.device)
+    else:
+        _rows(out, "out", T, H, dtype)
+    if w4:
+        st = lib().ss_embed_w4(_ptr(tokens), T, table._ref, scale, _ptr(out), _dtype_code(out), _ld(out), _stream())
+    else:
+        st = lib().ss_embed(_ptr(tokens), T, _ptr(table), _dtype_code(table), V, H, _ld(table), scale, _ptr(out),
+                            _dtype_code(out), _ld(out), _stream())
+    _check(st)
+    return out
+
+
+def embed_grad_workspace(T, V, H, device="cuda"):
+    """A workspace for ``embed_grad`` of these sizes."""
+    n = int(lib().ss_embed_grad_bytes(T, V, H))
+    if n == 0:
+        raise SSError("invalid sizes for workspace")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def embed_grad(dout, tokens, V, scale=1.0, out=None, dtype=torch.float32, accumulate=False, ws=None):
+    """The table's gradient [V, H] of ``embed``: scale * the sum of dout [T, H] over each token's positions.
+    ``accumulate`` adds it to ``out`` and leaves the rows that no token names as they were."""
+    _rows(dout, "dout")
+    T, H = dout.shape
+    if _tokens(tokens) != T:
+        raise SSError("tokens and dout must have as many rows")
+    if out is None:
+        if accumulate:
+            raise SSError("accumulate needs out")
+        out = torch.empty(V, H, dtype=dtype, device=dout.device)
+    else:
+        _rows(out, "out", V, H)
+    if ws is None:
+        ws = embed_grad_workspace(T, V, H, dout.device)
+    _here(ws, "ws")
+    _check(lib().ss_embed_grad(_ptr(dout), _dtype_code(dout), T, _ld(dout), _ptr(tokens), V, H, scale, _ptr(out),
+                               _dtype_code(out), _ld(out), accumulate, _ptr(ws), ws.numel() * ws.element_size(),
+                               _stream()))
+    return out
 
 
 def logits_tensor(d, device="cuda"):

@@ -18,7 +18,7 @@ OBJ_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libss.so")
 # measurement aid of bench.py (a plain streaming read), kept out of libss.so
 BENCH_LIB_PATH = os.path.join(HERE, "libss_bench.so")
-HEADERS = [os.path.join(CSRC, h) for h in ("ss_impl.hpp", "ss_row.hpp", "ss_device.hpp", "ss_launch.hpp")] + [
+HEADERS = [os.path.join(CSRC, h) for h in ("ss_impl.hpp", "ss_row.hpp", "ss_device.hpp", "ss_launch.hpp", "ss_w4.hpp")] + [
     os.path.join(ROOT, "include", "ss.h")
 ]
 
@@ -42,6 +42,9 @@ def units() -> list[tuple[str, str, list[str]]]:
         ("ss_stream", "ss_stream.hip", []),
         ("ss_aux", "ss_aux.hip", []),
         ("ss_noalloc", "ss_noalloc.hip", []),
+        ("ss_head", "ss_head.hip", []),
+        ("ss_embed", "ss_embed.hip", []),
+        ("ss_quant", "ss_quant.hip", []),
     ]
     for dn, dv in _DT.items():
         for on, ov in _OP.items():

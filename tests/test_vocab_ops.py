@@ -1,0 +1,719 @@
+"""The operators at the two ends of the vocabulary (4-bit head, lookup, its gradient, quantiser):
+small cases against plain implementations in 64 bits, refusals, and a run of them together.
+
+Tolerances.  A rounding to a type is off by at most half a step, u = eps / 2 relative.  The head's
+products are exact; a matrix instruction adds 32 of them, and a row is H / 32 (float32 hidden states:
+3 H / 32) instructions and at most 8 joins long, each addition off by at most 2^-23 of the sum of
+magnitudes S, whether it rounds or cuts: (32 + P H / 32 + 8) 2^-23 S.  The gradient's sums of n rows
+are n additions of float32, 2^-24 each.
+"""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+U = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+BF16, F32 = torch.bfloat16, torch.float32
+KINDS = [("int", 128), ("int", 64), ("int", 32), ("mx", 32)]
+E2M1 = np.array([0, .5, 1, 1.5, 2, 3, 4, 6, -0., -.5, -1, -1.5, -2, -3, -4, -6])
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+# ---------------------------------------------------------------------------
+# Plain implementations (numpy, 64 bits)
+# ---------------------------------------------------------------------------
+def pack(n, fmt):
+    """Dwords of codes n [V, H] (sign and magnitude in four bits: s mmm), by the layout's words."""
+    V, H = n.shape
+    nb = (H + 127) // 128
+    out = np.zeros((V, nb * 16), np.uint32)
+    for k in range(H):
+        b, c = divmod(k, 128)
+        j, g, e = c // 32, c % 32 // 8, c % 8
+        x = n[:, k].astype(np.uint64)
+        if fmt == "mx":
+            w = x << np.uint64(4 * e)
+        else:
+            byte = (x >> np.uint64(3)) << np.uint64(7) | x & np.uint64(7)
+            w = byte << np.uint64(8 * (e % 4))
+            if e >= 4:
+                w = w << np.uint64(4) | w >> np.uint64(28)
+        out[:, b * 16 + 4 * g + j] |= (w & np.uint64(0xFFFFFFFF)).astype(np.uint32)
+    return out.view(np.uint8).reshape(V, nb * 64)
+
+
+def numbers(n, fmt):
+    if fmt == "mx":
+        return E2M1[n]
+    m = (n & 7).astype(np.float64)
+    return np.where(n & 8, -m, m)
+
+
+def random_table(rng, V, H, fmt, group, fill=0xFF):
+    """(codes, scales) as the library takes them, and the table's values [V, H]; what pads the last block
+    is `fill`: it must not count."""
+    n = rng.integers(0, 16, (V, H)).astype(np.int64)
+    nb = (H + 127) // 128
+    codes = pack(n, fmt)
+    pad = nb * 128 - H
+    if pad:
+        junk = np.full((V, nb * 128), 15, np.int64)
+        junk[:, :H] = n
+        codes = pack(junk, fmt)
+    groups, padded = H // group, nb * 128 // group
+    if fmt == "mx":
+        x = rng.integers(115, 125, (V, padded)).astype(np.uint8)
+        x[:, groups:] = fill
+        s = np.exp2(x[:, :groups].astype(np.float64) - 127)
+        scales = torch.from_numpy(x)
+    else:
+        sc = torch.from_numpy(rng.uniform(0.001, 0.02, (V, padded)).astype(np.float32)).to(BF16)
+        sc[:, groups:] = float("nan")
+        s = sc[:, :groups].double().numpy()
+        scales = sc
+    return torch.from_numpy(codes), scales, numbers(n, fmt) * np.repeat(s, group, 1)
+
+
+def quantise(w, fmt, group):
+    """(codes n [V, H] s mmm, scales [V, H / group]) by the definition, in 64 bits."""
+    V, H = w.shape
+    x = w.astype(np.float64).reshape(V, -1, group)
+    with np.errstate(all="ignore"):
+        top = np.abs(x).max(2)
+        fine = np.isfinite(top)
+        if fmt == "int":
+            s = torch.from_numpy(np.where(fine, top, 0) / 7).float().to(BF16).double().numpy()
+            q = np.abs(x) / s[:, :, None]
+            m = np.where(s[:, :, None] > 0, np.minimum(np.rint(q), 7), 0)
+        else:
+            e = np.where(top > 0, np.floor(np.log2(np.where(fine & (top > 0), top, 1))), -1000)
+            s = np.exp2(np.maximum(e - 2, -127))
+            q = np.abs(x) / s[:, :, None]
+            half = np.array([.25, .75, 1.25, 1.75, 2.5, 3.5, 5.0])
+            up, down = (q[..., None] >= half).sum(-1), (q[..., None] > half).sum(-1)
+            m = np.where(up % 2 == 0, up, down)
+        m = np.where(fine[:, :, None], m, 0).astype(np.int64)
+        n = m | np.where(np.signbit(x) & fine[:, :, None], 8, 0)
+    return n.reshape(V, H), np.where(fine, s, np.nan)
+
+
+def as64(t):
+    return t.detach().double().cpu().numpy()
+
+
+# ---------------------------------------------------------------------------
+# Without a GPU: layout, sizes, refusals
+# ---------------------------------------------------------------------------
+@pytest.fixture(scope="module")
+def lib():
+    import os
+
+    from paper_2607_20475_amd import build as b
+    if not os.path.exists(b.LIB_PATH):
+        b.build()
+    from paper_2607_20475_amd import binding
+    return binding.lib()
+
+
+def test_layout_of_the_performance_cases_is_the_documented_one():
+    """The plain form's packing and values (what perf/operators.py feeds to both sides)."""
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "perf", "operators.py")
+    spec = importlib.util.spec_from_file_location("perf_operators", path)
+    M = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(M)
+    rng = np.random.default_rng(0)
+    for fmt, group in KINDS:
+        w = rng.normal(0, 0.02, (9, 3 * 128 + max(group, 32))).astype(np.float32)[:, : 3 * 128 + group % 128]
+        n, s = quantise(w, fmt, group)
+        codes, scales = M._quantise(torch.from_numpy(w), fmt, group)
+        assert np.array_equal(codes.numpy(), pack(n, fmt)), (fmt, group)
+        v = M._values(codes, scales, fmt, group, w.shape[1])
+        assert np.array_equal(as64(v), numbers(n, fmt) * np.repeat(s, group, 1))
+
+
+def test_table_sizes(lib):
+    from paper_2607_20475_amd import binding as b
+    size = lambda V, H, fmt, group: (  # noqa: E731
+        lib.ss_w4_codes_bytes(C.byref(b._W4(V=V, H=H, fmt=fmt, group=group))),
+        lib.ss_w4_scales_bytes(C.byref(b._W4(V=V, H=H, fmt=fmt, group=group))))
+    assert size(10, 256, 0, 128) == (10 * 128, 10 * 4)
+    assert size(10, 160, 0, 32) == (10 * 128, 10 * 16)
+    assert size(10, 160, 1, 32) == (10 * 128, 10 * 8)
+    assert size(1 << 20, 8192, 1, 32) == (1 << 32, 1 << 28)
+    for bad in [(0, 256, 0, 128), ((1 << 20) + 1, 256, 0, 128), (10, 0, 0, 128), (10, 192, 0, 128), (10, 96, 0, 64),
+                (10, 40, 0, 32), (10, 256, 0, 16), (10, 256, 1, 64), (10, 48, 1, 32), (10, 256, 2, 32),
+                (10, (1 << 16) + 128, 0, 128), (-1, 256, 0, 128)]:
+        assert size(*bad) == (0, 0), bad
+    assert lib.ss_w4_codes_bytes(None) == 0
+
+
+def test_head_arguments_are_checked_before_launch(lib):
+    from paper_2607_20475_amd import binding as b
+    fake = 0x10000  # never dereferenced: validation fails first
+
+    def call(h=fake, dtype=1, T=4, ld_h=256, V=100, H=256, fmt=0, group=128, codes=fake, scales=fake, out=fake,
+             out_dtype=1, ld=100, ws=fake, ws_bytes=1 << 20):
+        t = b._W4(V=V, H=H, fmt=fmt, group=group, codes=codes, scales=scales)
+        return lib.ss_head_w4(h, dtype, T, ld_h, C.byref(t), out, out_dtype, ld, ws, ws_bytes, None)
+
+    for bad in [dict(h=None), dict(dtype=2), dict(T=-1), dict(T=(1 << 20) + 1), dict(ld_h=255), dict(V=0), dict(H=192),
+                dict(fmt=3), dict(group=16), dict(codes=None), dict(codes=fake + 8), dict(scales=None),
+                dict(scales=fake + 2), dict(out=None), dict(out_dtype=-1), dict(ld=99), dict(ws=None)]:
+        assert call(**bad) == -1, bad
+    assert lib.ss_head_w4(fake, 1, 4, 256, None, fake, 1, 100, fake, 1 << 20, None) == -1
+    n = lib.ss_head_w4_bytes(4, 256, 0)
+    assert call(dtype=0, ws_bytes=n - 1) == -3
+    assert call(ws=fake + 8) == -3
+    assert call(T=0, h=None, out=None, ws=None) == 0  # no rows: nothing to do
+    assert lib.ss_head_w4_bytes(-1, 256, 0) == 0 and lib.ss_head_w4_bytes(4, 0, 0) == 0
+    assert lib.ss_head_w4_bytes(4, 256, 2) == 0
+
+
+def test_lookup_arguments_are_checked_before_launch(lib):
+    from paper_2607_20475_amd import binding as b
+    fake = 0x10000
+
+    def call(tokens=fake, T=4, table=fake, dtype=1, V=100, H=60, ld=60, out=fake, out_dtype=0, ld_out=60):
+        return lib.ss_embed(tokens, T, table, dtype, V, H, ld, 1.0, out, out_dtype, ld_out, None)
+
+    for bad in [dict(tokens=None), dict(T=-1), dict(T=(1 << 20) + 1), dict(table=None), dict(dtype=2), dict(V=0),
+                dict(H=0), dict(H=(1 << 16) + 1), dict(ld=59), dict(out=None), dict(out_dtype=5), dict(ld_out=59)]:
+        assert call(**bad) == -1, bad
+    assert call(T=0, tokens=None, table=None, out=None) == 0
+    t = b._W4(V=100, H=256, fmt=0, group=128, codes=fake, scales=fake)
+    assert lib.ss_embed_w4(fake, 4, C.byref(t), 1.0, fake, 0, 255, None) == -1
+    assert lib.ss_embed_w4(None, 4, C.byref(t), 1.0, fake, 0, 256, None) == -1
+    assert lib.ss_embed_w4(fake, 4, None, 1.0, fake, 0, 256, None) == -1
+    assert lib.ss_embed_w4(None, 0, C.byref(t), 1.0, None, 0, 256, None) == 0
+    t.codes = fake + 4
+    assert lib.ss_embed_w4(fake, 4, C.byref(t), 1.0, fake, 0, 256, None) == -1
+
+
+def test_gradient_arguments_are_checked_before_launch(lib):
+    fake = 0x10000
+    n = lib.ss_embed_grad_bytes(4, 100, 60)
+
+    def call(dout=fake, dtype=1, T=4, ld=60, tokens=fake, V=100, H=60, out=fake, out_dtype=0, ld_out=60, ws=fake,
+             ws_bytes=n):
+        return lib.ss_embed_grad(dout, dtype, T, ld, tokens, V, H, 1.0, out, out_dtype, ld_out, 0, ws, ws_bytes, None)
+
+    for bad in [dict(dout=None), dict(dtype=2), dict(T=-1), dict(T=(1 << 20) + 1), dict(ld=59), dict(tokens=None),
+                dict(V=0), dict(V=(1 << 20) + 1), dict(H=0), dict(out=None), dict(out_dtype=2), dict(ld_out=59),
+                dict(ws=None)]:
+        assert call(**bad) == -1, bad
+    assert call(ws_bytes=n - 1) == -3
+    assert call(ws=fake + 4) == -3
+    assert lib.ss_embed_grad_bytes(4, 0, 60) == 0 and lib.ss_embed_grad_bytes(-1, 10, 60) == 0
+
+
+def test_quantiser_arguments_are_checked_before_launch(lib):
+    from paper_2607_20475_amd import binding as b
+    fake = 0x10000
+
+    def call(w=fake, dtype=1, ld=256, V=100, H=256, fmt=0, group=128, codes=fake, scales=fake, values=None, vdt=0, ldv=0):
+        t = b._W4(V=V, H=H, fmt=fmt, group=group, codes=codes, scales=scales)
+        return lib.ss_quant_w4(w, dtype, ld, C.byref(t), values, vdt, ldv, None)
+
+    for bad in [dict(w=None), dict(dtype=2), dict(ld=255), dict(V=0), dict(H=100), dict(fmt=2), dict(group=8),
+                dict(codes=None), dict(scales=None), dict(codes=fake + 1), dict(values=fake, ldv=255),
+                dict(values=fake, vdt=3, ldv=256)]:
+        assert call(**bad) == -1, bad
+
+
+def test_wrappers_refuse_what_they_cannot_pass_on():
+    from paper_2607_20475_amd import binding as b
+    with pytest.raises(b.SSError, match="neither"):
+        b.W4.empty(4, 128, "fp8", 128, device="cpu")
+    with pytest.raises(b.SSError, match="no int table"):
+        b.W4.empty(4, 192, "int", 128, device="cpu")
+    t = b.W4.empty(4, 160, "int", 32, device="cpu")
+    assert t.codes.shape == (4, 128) and t.scales.shape == (4, 8)
+    with pytest.raises(b.SSError, match="codes"):
+        b.W4(t.codes[:, :64], t.scales, 4, 160, "int", 32)
+    with pytest.raises(b.SSError, match="scales"):
+        b.W4(t.codes, t.scales.float(), 4, 160, "int", 32)
+    with pytest.raises(b.SSError, match="not on a GPU"):
+        b.head_w4(torch.zeros(2, 160, dtype=BF16), t)
+    with pytest.raises(b.SSError, match="not on a GPU"):
+        b.embed(torch.zeros(2, dtype=torch.int32), t)
+    with pytest.raises(b.SSError, match="tokens"):
+        b.embed(torch.zeros(2, dtype=torch.int64), t)
+    with pytest.raises(b.SSError, match="unit column stride"):
+        b.embed_grad(torch.zeros(6, 4).t(), torch.zeros(4, dtype=torch.int32), 10)
+    with pytest.raises(b.SSError, match="unit column stride"):  # broadcast rows
+        b.embed_grad(torch.zeros(1, 6).expand(4, 6), torch.zeros(4, dtype=torch.int32), 10)
+
+
+# ---------------------------------------------------------------------------
+# On the GPU
+# ---------------------------------------------------------------------------
+@pytest.fixture(scope="module")
+def ssb():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2607_20475_amd import binding
+    binding.lib()
+    return binding
+
+
+def strided(t, extra, shift=0):
+    """t on the GPU as rows `extra` columns further apart, `shift` elements into an allocation of sentinels."""
+    R, n = t.shape
+    base = torch.full((R * (n + extra) + shift + 8,), 77.0, dtype=t.dtype, device="cuda")
+    v = base[shift:shift + R * (n + extra)].view(R, n + extra)
+    v[:, :n] = t.cuda()
+    return v[:, :n], base
+
+
+HEAD = [
+    # T, V, H: one token and one row, tiles that end inside, every number of token tiles, partial blocks
+    (1, 1, 32), (1, 65, 128), (2, 15, 64), (3, 16, 96), (5, 63, 160), (15, 64, 384), (16, 257, 640), (16, 1000, 1152),
+    (17, 70, 128), (31, 300, 224), (32, 64, 256), (33, 257, 288), (48, 130, 512), (50, 513, 640), (64, 256, 384),
+    (65, 259, 96), (100, 1025, 256), (129, 33, 1056), (200, 2100, 128), (1, 5000, 2048), (7, 40, 8192), (40, 20, 8192),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", KINDS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_head_against_64_bits(ssb, fmt, group, dtype):
+    rng = np.random.default_rng(31 + group)
+    for i, (T, V, H) in enumerate(HEAD):
+        if H % group:
+            H = (H + group - 1) // group * group
+        codes, scales, W = random_table(rng, V, H, fmt, group)
+        table = ssb.W4(codes.cuda(), scales.cuda(), V, H, fmt, group)
+        h = torch.from_numpy(rng.normal(0, 1, (T, H)).astype(np.float32)).to(dtype)
+        for out_dtype, extra, shift in ((BF16, 0, 0), (F32, 3, 1), (BF16, 4, 4)):
+            say(f"[head] {fmt}{group} {dtype} T={T} V={V} H={H} out={out_dtype} extra={extra}")
+            hs, _ = strided(h, extra, shift)
+            out, base = strided(torch.zeros(T, V, dtype=out_dtype), extra, shift)
+            r = ssb.head_w4(hs, table, out=out)
+            torch.cuda.synchronize()
+            assert r.data_ptr() == out.data_ptr()
+            h64 = as64(h)
+            ref, S = h64 @ W.T, np.abs(h64) @ np.abs(W).T
+            P = 3 if dtype == F32 else 1
+            tol = (32 + P * H / 32 + 8) * 2.0 ** -23 * S * (1 + U[out_dtype]) + U[out_dtype] * np.abs(ref) + 1e-30
+            err = np.abs(as64(out) - ref)
+            assert (err <= tol).all(), (T, V, H, out_dtype, float((err / tol).max()))
+            rest = base[shift:shift + T * (V + extra)].view(T, V + extra)[:, V:]
+            assert (rest == 77).all() and (base[:shift] == 77).all() and (base[shift + T * (V + extra):] == 77).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 40])
+def test_head_takes_float32_whole(ssb, T):
+    """Hidden states that differ beyond bfloat16: the result keeps what float32 has.  A table row of a single one
+    returns the state itself, bit for bit."""
+    rng = np.random.default_rng(2)
+    V, H = 256, 256
+    n = np.zeros((V, H), np.int64)
+    n[np.arange(V), np.arange(V)] = 1
+    one = torch.ones(V, 2, dtype=BF16)
+    table = ssb.W4(torch.from_numpy(pack(n, "int")).cuda(), one.cuda(), V, H, "int", 128)
+    h = (rng.normal(0, 1, (T, H)) * np.exp2(rng.integers(-60, 60, (T, H)))).astype(np.float32)
+    out = ssb.head_w4(torch.from_numpy(h).cuda(), table)
+    assert np.array_equal(out.cpu().numpy(), h)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [4, 70])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_head_keeps_rows_and_columns_apart(ssb, T, dtype):
+    """Infinities and NaN of one hidden row or one table row stay there."""
+    rng = np.random.default_rng(3)
+    for fmt, group in KINDS:
+        V, H = 130, 256
+        codes, scales, W = random_table(rng, V, H, fmt, group)
+        if fmt == "mx":
+            scales[77, 3] = 255
+        else:
+            scales[77, 0] = float("nan")
+        h = torch.from_numpy(rng.normal(0, 1, (T, H)).astype(np.float32)).to(dtype)
+        h[1, 5], h[2, 9], h[T - 1, 0] = float("inf"), float("nan"), -float("inf")
+        out = ssb.head_w4(h.cuda(), ssb.W4(codes.cuda(), scales.cuda(), V, H, fmt, group), dtype=F32)
+        got = torch.isfinite(out).cpu().numpy()
+        want = np.ones((T, V), bool)
+        want[:, 77] = False
+        want[[1, 2, T - 1]] = False
+        assert np.array_equal(got, want), (fmt, group)
+        assert torch.isnan(out[2]).all()
+
+
+@pytest.mark.gpu
+def test_head_extreme_scales(ssb):
+    """Powers of two over the range that bfloat16 has as normal numbers, and integer scales down to its subnormals."""
+    V, H = 16, 64
+    n = np.full((V, H), 2, np.int64)  # 1.0 in E2M1, 2 as an integer
+    x = np.tile(np.array([[2, 3, 20, 60, 100, 126, 127, 128, 150, 180, 200, 220, 240, 250, 251, 247]], np.uint8).T, (1, 4))
+    h = torch.ones(1, H, dtype=BF16)
+    out = ssb.head_w4(h.cuda(), ssb.W4(torch.from_numpy(pack(n, "mx")).cuda(), torch.from_numpy(x).cuda(), V, H, "mx", 32),
+                      dtype=F32)
+    with np.errstate(over="ignore"):  # 64 * 2^123 and 64 * 2^124 are infinities in float32, as in the result
+        assert np.array_equal(out.cpu().numpy()[0], (H * np.exp2(x[:, 0].astype(np.float64) - 127)).astype(np.float32))
+    s = torch.from_numpy(np.exp2(np.linspace(-133, 110, V).round())).to(BF16)[:, None].repeat(1, 2)
+    out = ssb.head_w4(h.cuda(), ssb.W4(torch.from_numpy(pack(n, "int")).cuda(), s.cuda(), V, H, "int", 64), dtype=F32)
+    assert np.array_equal(as64(out)[0], as64(s)[:, 0] * 2 * H)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("out_dtype", [BF16, F32])
+def test_lookup_against_64_bits(ssb, dtype, out_dtype):
+    rng = np.random.default_rng(5)
+    for T, V, H, extra, shift in [(1, 1, 1, 0, 0), (5, 7, 8, 0, 0), (9, 33, 100, 3, 1), (64, 50, 2048, 0, 0),
+                                  (33, 1000, 2049, 0, 0), (300, 20, 4104, 8, 8), (2, 3, 5000, 1, 3)]:
+        table = torch.from_numpy(rng.normal(0, 1, (V, H)).astype(np.float32)).to(dtype)
+        tok = rng.integers(0, V, T).astype(np.int32)
+        tok[rng.random(T) < 0.2] = -1
+        tok[-1] = V - 1
+        if T > 3:
+            tok[:3] = V, 2 ** 31 - 1, -2 ** 31
+        say(f"[lookup] {dtype}->{out_dtype} T={T} V={V} H={H} extra={extra}")
+        tt, _ = strided(table, extra, shift)
+        out, base = strided(torch.zeros(T, H, dtype=out_dtype), extra, shift)
+        ssb.embed(torch.from_numpy(tok).cuda(), tt, scale=1.5, out=out)
+        there = (tok >= 0) & (tok < V)
+        ref = np.where(there[:, None], as64(table)[np.where(there, tok, 0)] * 1.5, 0)
+        # one product rounded to float32, one rounding to the output
+        assert (np.abs(as64(out) - ref) <= np.abs(ref) * (U[out_dtype] + 2.0 ** -24 * (1 + U[out_dtype]))).all()
+        rest = base[shift:shift + T * (H + extra)].view(T, H + extra)[:, H:]
+        assert (rest == 77).all() and (base[:shift] == 77).all() and (base[shift + T * (H + extra):] == 77).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", KINDS)
+def test_lookup_in_4_bits(ssb, fmt, group):
+    rng = np.random.default_rng(6)
+    for T, V, H, out_dtype in [(1, 1, group, F32), (40, 9, 3 * 128 + group % 128, BF16), (300, 77, 4096, F32),
+                               (5, 600, 2944, BF16)]:
+        codes, scales, W = random_table(rng, V, H, fmt, group)
+        table = ssb.W4(codes.cuda(), scales.cuda(), V, H, fmt, group)
+        tok = rng.integers(-2, V + 2, T).astype(np.int32)
+        say(f"[lookup] {fmt}{group} T={T} V={V} H={H}")
+        out = ssb.embed(torch.from_numpy(tok).cuda(), table, scale=0.3, dtype=out_dtype)
+        there = (tok >= 0) & (tok < V)
+        ref = np.where(there[:, None], W[np.where(there, tok, 0)] * float(np.float32(0.3)), 0)
+        assert (np.abs(as64(out) - ref) <= np.abs(ref) * (U[out_dtype] + 2.0 ** -24 * (1 + U[out_dtype]))).all()
+
+
+def grad64(dout, tok, V, scale):
+    ref, S, n = np.zeros((V, dout.shape[1])), np.zeros((V, dout.shape[1])), np.zeros(V)
+    for t, v in enumerate(tok):
+        if 0 <= v < V:
+            ref[v] += dout[t] * scale
+            S[v] += np.abs(dout[t] * scale)
+            n[v] += 1
+    return ref, S, n
+
+
+GRAD = [
+    # T, V, H, how the tokens fall
+    (0, 5, 16, "even"), (1, 1, 1, "even"), (1, 300, 8, "even"), (7, 513, 60, "even"), (128, 4, 64, "even"),
+    (129, 2, 72, "one"), (500, 257, 100, "few"), (1000, 700, 40, "zipf"), (1000, 3, 2056, "few"), (640, 256, 33, "blocks"),
+    (3000, 40, 24, "zipf"), (2500, 1, 16, "one"), (300, 600, 16, "none"), (1025, 1025, 8, "even"), (5000, 9000, 16, "sorted"),
+]
+
+
+def grad_tokens(rng, T, V, how):
+    if how == "one":
+        return np.full(T, V - 1, np.int32)
+    if how == "none":
+        return rng.choice(np.array([-1, V, 2 ** 31 - 1, -2 ** 31], np.int64), T).astype(np.int32)
+    if how == "few":
+        tok = rng.integers(0, min(V, 3), T)
+    elif how == "zipf":
+        tok = np.minimum((np.exp(rng.random(T) * np.log(V + 1)) - 1).astype(np.int64), V - 1)
+    elif how == "blocks":  # runs of exactly 128 and its neighbours
+        tok = np.repeat(np.arange(5), [128, 129, 127, 128, 128])[:T]
+    else:
+        tok = rng.integers(0, V, T)
+    if how == "sorted":
+        tok = np.sort(tok)
+    tok = tok.astype(np.int32)
+    if how != "blocks":
+        tok[rng.random(T) < 0.1] = -1
+    return tok
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("out_dtype", [BF16, F32])
+def test_gradient_against_64_bits(ssb, dtype, out_dtype):
+    rng = np.random.default_rng(7)
+    for i, (T, V, H, how) in enumerate(GRAD):
+        dout = torch.from_numpy(rng.normal(0, 1, (T, H)).astype(np.float32)).to(dtype)
+        tok = grad_tokens(rng, T, V, how)
+        extra, shift = (0, 0) if i % 2 else (3, 1)
+        say(f"[grad] {dtype}->{out_dtype} T={T} V={V} H={H} {how} extra={extra}")
+        ref, S, n = grad64(as64(dout), tok, V, 0.75)
+        slack = (n[:, None] + 2) * 2.0 ** -24 * S
+        ds, _ = strided(dout, extra, shift)
+        t = torch.from_numpy(tok).cuda()
+        out, base = strided(torch.full((V, H), 5.0, dtype=out_dtype), extra, shift)
+        ssb.embed_grad(ds, t, V, scale=0.75, out=out)
+        err = np.abs(as64(out) - ref)
+        tol = slack * (1 + U[out_dtype]) + U[out_dtype] * np.abs(ref)
+        assert (err <= tol).all(), (T, V, H, how)
+        rest = base[shift:shift + V * (H + extra)].view(V, H + extra)[:, H:]
+        assert (rest == 77).all() and (base[:shift] == 77).all() and (base[shift + V * (H + extra):] == 77).all()
+        # the same call, the same bits; added to what is there, the rows without a token untouched
+        again = ssb.embed_grad(ds, t, V, scale=0.75, dtype=out_dtype)
+        assert torch.equal(again, out)
+        start = torch.from_numpy(rng.normal(0, 1, (V, H)).astype(np.float32)).to(out_dtype)
+        start[n == 0] = float("nan")
+        acc = start.cuda()
+        ssb.embed_grad(ds, t, V, scale=0.75, out=acc, accumulate=True)
+        keep = torch.from_numpy(n == 0)
+        assert torch.isnan(acc.cpu()[keep]).all()
+        sum64 = as64(start)[n > 0] + ref[n > 0]
+        tol = ((slack[n > 0] + 2.0 ** -24 * np.abs(sum64)) * (1 + U[out_dtype]) + U[out_dtype] * np.abs(sum64)) * (1 + 2 ** -20)
+        assert (np.abs(as64(acc)[n > 0] - sum64) <= tol).all(), (T, V, H, how)
+
+
+@pytest.mark.gpu
+def test_gradient_is_the_lookups(ssb):
+    """<lookup(W + E) - lookup(W), d> = <E, gradient(d)>: the lookup is linear, so the difference is exact but for
+    rounding (small integers: none at all)."""
+    rng = np.random.default_rng(8)
+    T, V, H = 400, 90, 96
+    W, E = (torch.from_numpy(rng.integers(-8, 9, (V, H)).astype(np.float32)).cuda() for _ in range(2))
+    d = torch.from_numpy(rng.integers(-8, 9, (T, H)).astype(np.float32)).cuda()
+    tok = torch.from_numpy(grad_tokens(rng, T, V, "zipf")).cuda()
+    diff = ssb.embed(tok, W + E, scale=0.5) - ssb.embed(tok, W, scale=0.5)
+    assert float((diff.double() * d.double()).sum()) == float(
+        (E.double() * ssb.embed_grad(d, tok, V, scale=0.5).double()).sum())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", KINDS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_quantiser_by_its_definition(ssb, fmt, group, dtype):
+    rng = np.random.default_rng(9)
+    for V, H, extra, shift in [(1, group, 0, 0), (50, 3 * 128 + group % 128, 3, 1), (257, 1024, 8, 8), (3, 4096, 0, 0)]:
+        w = rng.normal(0, 0.02, (V, H)).astype(np.float32)
+        if V >= 50:
+            w[3] = 0
+            w[4, : group] = 1e-44
+            w[5] *= 1e-36
+            w[6] *= 1e38
+            w[7] *= np.exp2(-100.0).astype(np.float32)
+            w[8, 5], w[9, H - 1], w[10, 0] = np.nan, np.inf, -np.inf
+            # ties: halves of a scale of one, and numbers next to them
+            w[11] = rng.choice(np.arange(-7, 7.5, 0.5), H)
+            w[11, ::group] = 7
+            w[12] = np.nextafter(w[11], np.float32(100))
+            w[12, ::group] = 7
+            w[13] = np.nextafter(w[11], np.float32(-100))
+            w[13, ::group] = 7
+            w[14] = rng.choice(np.array([0, .25, .75, 1.25, 1.75, 2.5, 3.5, 5, 6, 7, 7.9], np.float32), H)
+            w[15] = -np.abs(w[15])
+            w[16] = rng.integers(-200, 200, H) * np.float32(0.37)
+        w = torch.from_numpy(w).to(dtype)
+        n, s = quantise(w.double().numpy(), fmt, group)
+        ws, _ = strided(w, extra, shift)
+        for values_dtype in (None, F32, BF16):
+            say(f"[quant] {fmt}{group} {dtype} V={V} H={H} values={values_dtype}")
+            table = ssb.W4.empty(V, H, fmt, group)
+            table.codes.fill_(0x55)
+            values, base = (None, None) if values_dtype is None else strided(torch.zeros(V, H, dtype=values_dtype), extra, shift)
+            assert ssb.quantize_w4(ws, table, values=values) is table
+            assert np.array_equal(table.codes.cpu().numpy(), pack(n, fmt)), np.nonzero((table.codes.cpu().numpy() != pack(n, fmt)).any(1))
+            got = table.scales.cpu()
+            got = np.where(got.numpy() == 255, np.nan, np.exp2(got.double().numpy() - 127)) if fmt == "mx" else as64(got)
+            assert np.array_equal(got[:, : H // group], s, equal_nan=True)
+            if values is not None:
+                exact = torch.from_numpy(numbers(n, fmt) * np.repeat(s, group, 1))
+                assert torch.equal(torch.nan_to_num(values.cpu().double(), nan=9e9), torch.nan_to_num(
+                    exact.float().to(values_dtype).double(), nan=9e9))
+                rest = base[shift:shift + V * (H + extra)].view(V, H + extra)[:, H:]
+                assert (rest == 77).all()
+        new = ssb.quantize_w4(ws, fmt=fmt, group=group)
+        assert torch.equal(new.codes, table.codes)
+
+
+@pytest.mark.gpu
+def test_wrappers_refuse_on_the_gpu(ssb):
+    t = ssb.W4.empty(64, 256, "int", 128)
+    h = torch.zeros(4, 256, dtype=BF16, device="cuda")
+    tok = torch.zeros(4, dtype=torch.int32, device="cuda")
+    for call in [lambda: ssb.head_w4(h[:, :128], t), lambda: ssb.head_w4(h.half(), t),
+                 lambda: ssb.head_w4(h, t, out=torch.zeros(4, 63, dtype=BF16, device="cuda")),
+                 lambda: ssb.head_w4(h, t, out=torch.zeros(64, 4, dtype=BF16, device="cuda").t()),
+                 lambda: ssb.head_w4(h, t, ws=torch.zeros(16, dtype=torch.uint8, device="cuda")),
+                 lambda: ssb.embed(tok[::2], t), lambda: ssb.embed(tok.long(), t),
+                 lambda: ssb.embed(tok, t, out=torch.zeros(4, 256, dtype=torch.float16, device="cuda")),
+                 lambda: ssb.embed_grad(h, tok[:3], 10), lambda: ssb.embed_grad(h, tok, 10, accumulate=True),
+                 lambda: ssb.embed_grad(h, tok, 10, ws=torch.zeros(16, dtype=torch.uint8, device="cuda")),
+                 lambda: ssb.quantize_w4(h, t), lambda: ssb.quantize_w4(h[:, :100], fmt="mx", group=32)]:
+        with pytest.raises(ssb.SSError):
+            call()
+
+
+@pytest.mark.gpu
+def test_no_rows(ssb):
+    t = ssb.W4.empty(64, 256, "int", 128)
+    e = torch.zeros(0, dtype=torch.int32, device="cuda")
+    assert ssb.head_w4(torch.zeros(0, 256, dtype=BF16, device="cuda"), t).shape == (0, 64)
+    assert ssb.embed(e, t).shape == (0, 256)
+    out = torch.full((10, 256), 3.0, device="cuda")
+    ssb.embed_grad(torch.zeros(0, 256, device="cuda"), e, 10, out=out, accumulate=True)
+    assert (out == 3).all()
+    ssb.embed_grad(torch.zeros(0, 256, device="cuda"), e, 10, out=out)
+    assert (out == 0).all()
+
+
+def loop_inputs(ssb, B, V, H, fmt, group):
+    """A table, its 4-bit form, and sampling parameters: greedy and stochastic requests side by side."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(12)
+    W = torch.empty(V, H, dtype=BF16, device="cuda").normal_(0, 0.05, generator=g)
+    mode = torch.where(torch.arange(B, device="cuda") % 2 == 0, ssb.GREEDY, ssb.TEMP | ssb.TOPK).to(torch.int32)
+    prm = ssb.Params(B, V, mode=mode, temperature=torch.full((B,), 0.7, device="cuda"),
+                     top_k=torch.full((B,), 20, dtype=torch.int32, device="cuda"),
+                     seed=torch.arange(B, device="cuda"), position=torch.zeros(B, dtype=torch.int64, device="cuda"))
+    return W, ssb.quantize_w4(W, fmt=fmt, group=group), prm
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group,B", [("int", 128, 8), ("mx", 32, 24)])
+def test_decode_loop_eager_and_replayed(ssb, fmt, group, B):
+    """Lookup, (an identity for the model,) head, sampler, and again; the loop captured in a graph gives the same
+    tokens on every replay, with eager work between them."""
+    V, H, steps = 3000, 512, 3
+    W, table, prm = loop_inputs(ssb, B, V, H, fmt, group)
+    first = torch.arange(B, dtype=torch.int32, device="cuda") * 7
+    ws = ssb.workspace(ssb.OP_SAMPLE, B, V, 0, 64, ssb.F32)
+    hws = ssb.head_workspace(torch.empty(B, H, dtype=BF16, device="cuda"))
+    logits = [torch.empty(B, V, device="cuda") for _ in range(steps)]
+
+    def loop():
+        tok, seen = first, []
+        for s in range(steps):
+            x = ssb.embed(tok, table, scale=4.0)
+            ssb.head_w4(x, table, out=logits[s], ws=hws)
+            tok = ssb.sample(logits[s], prm, 64, ws=ws)[0]
+            seen.append(tok)
+        return seen
+
+    say(f"[loop] eager {fmt}{group} B={B}")
+    want = [t.clone() for t in loop()]
+    torch.cuda.synchronize()
+    table64 = as64(ssb.embed(torch.arange(V, dtype=torch.int32, device="cuda"), table, dtype=F32))
+    tok = first.cpu().numpy()
+    for s in range(steps):  # greedy rows: the leading logit of the 64-bit product, up to its rounding
+        x = as64((torch.from_numpy(table64[tok] * 4)).to(BF16))
+        ref = x @ table64.T
+        got = want[s].cpu().numpy()
+        for b in range(0, B, 2):
+            assert ref[b, got[b]] >= ref[b].max() - 1e-4 * np.abs(ref[b]).max()
+        tok = got
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        loop()
+    torch.cuda.current_stream().wait_stream(side)
+    say("[loop] capture")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = loop()
+    for rep in range(3):
+        say(f"[loop] replay {rep}")
+        for t in got:
+            t.fill_(-5)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+        eager = loop()
+        assert all(torch.equal(a, b) for a, b in zip(want, eager))
+
+
+@pytest.mark.gpu
+def test_verification_takes_the_heads_logits(ssb):
+    """Draft rows through the head into ss_verify_sparse; its padded tokens through the lookup."""
+    B, L, V, H = 4, 3, 2500, 384
+    W, table, _ = loop_inputs(ssb, B, V, H, "int", 64)
+    prm = ssb.Params(B, V, mode=torch.full((B,), ssb.GREEDY, dtype=torch.int32, device="cuda"),
+                     seed=torch.arange(B, device="cuda"), position=torch.zeros(B, dtype=torch.int64, device="cuda"))
+    h = torch.empty(B * (L + 1), H, dtype=BF16, device="cuda").normal_()
+    logits = ssb.head_w4(h, table)
+    best = logits.float().argmax(1).view(B, L + 1)
+    draft = best[:, :L].clone()
+    draft[1, 1] = (draft[1, 1] + 1) % V  # request 1 is rejected at its second draft
+    tokens, n, _ = ssb.verify_sparse(logits.view(B, L + 1, V), draft[:, :, None].int().contiguous(),
+                                     torch.ones(B, L, 1, device="cuda"), draft.int().contiguous(), prm, 64)
+    assert n.tolist() == [3, 1, 3, 3]
+    rows = ssb.embed(tokens.view(-1), table, dtype=F32).view(B, L + 1, H)
+    assert (rows[1, 2:] == 0).all() and (rows[1, :2].abs().sum(1) > 0).all()
+    want = ssb.embed(best.int().view(-1), table, dtype=F32).view(B, L + 1, H)
+    assert torch.equal(rows[0], want[0]) and torch.equal(rows[1, :2], want[1, :2])
+
+
+@pytest.mark.gpu
+def test_training_step_refreshes_the_serving_table(ssb):
+    """Gradient, update, new 4-bit form: all captured, replayed twice; a plain 64-bit step beside it."""
+    T, V, H = 300, 400, 256
+    rng = np.random.default_rng(13)
+    W0 = torch.from_numpy(rng.normal(0, 0.05, (V, H)).astype(np.float32))
+    W = W0.cuda()
+    tok = grad_tokens(rng, T, V, "zipf")
+    t = torch.from_numpy(tok).cuda()
+    d = torch.from_numpy(rng.normal(0, 0.01, (T, H)).astype(np.float32))
+    dd = d.cuda()
+    table = ssb.W4.empty(V, H, "mx", 32)
+    gws, dW = ssb.embed_grad_workspace(T, V, H), torch.empty(V, H, device="cuda")
+
+    def step():
+        ssb.embed_grad(dd, t, V, scale=2.0, out=dW, ws=gws)
+        W.sub_(dW)
+        ssb.quantize_w4(W, table)
+        return ssb.embed(t, table, scale=2.0, dtype=F32)
+
+    step()
+    torch.cuda.synchronize()
+    W.copy_(W0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    ref = as64(W0)
+    g64 = grad64(as64(d), tok, V, 2.0)[0]
+    for rep in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        ref = ref - g64
+        assert np.abs(as64(W) - ref).max() <= 1e-5 * max(1, np.abs(ref).max())
+        n, s = quantise(W.cpu().numpy().astype(np.float64), "mx", 32)
+        vals = numbers(n, "mx") * np.repeat(s, 32, 1)
+        there = tok >= 0
+        assert np.array_equal(as64(out), np.where(there[:, None], vals[np.where(there, tok, 0)] * 2, 0))
+        torch.zeros(1000, device="cuda").sum()
+
+
+@pytest.mark.gpu
+def test_two_streams_with_their_own_workspaces(ssb):
+    rng = np.random.default_rng(14)
+    V, H = 5000, 1024
+    codes, scales, _ = random_table(rng, V, H, "int", 128)
+    table = ssb.W4(codes.cuda(), scales.cuda(), V, H, "int", 128)
+    hs = [torch.empty(T, H, device="cuda").normal_() for T in (5, 40)]
+    toks = [torch.randint(0, V, (700,), device="cuda", dtype=torch.int32) for _ in range(2)]
+    ds = [torch.empty(700, H, device="cuda").normal_() for _ in range(2)]
+    want = [(ssb.head_w4(h, table), ssb.embed_grad(d, t, V)) for h, d, t in zip(hs, ds, toks)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [None, None]
+    for rep in range(3):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = (ssb.head_w4(hs[i], table), ssb.embed_grad(ds[i], toks[i], V))
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
