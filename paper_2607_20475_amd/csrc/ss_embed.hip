@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void ss_embed_w4_kernel(EmbedArgs a) {
       s = mx_scale(a.scales[group]);
     else
       s = bf16_value(reinterpret_cast<const uint16_t*>(a.scales)[group]);
-    const uint4 e = w4_expand<KIND>(word, 1.0f);  // codes: exact
+    const u32x4 e = w4_expand<KIND>(word, 1.0f);  // codes: exact
     const uint32_t u[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {

@@ -19,6 +19,7 @@ namespace ss {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -66,9 +67,10 @@ __device__ __forceinline__ uint32_t as_u32(bf16x2 v) { return __builtin_bit_cast
 //   in bfloat16.  Seven instructions for eight elements (four for E2M1).  The
 //   group's scale is left to the caller: a product of integer and scale has up
 //   to 11 bits and would be rounded in bfloat16, the sum over a group is scaled in float32.
+// `scale` (E2M1) is mx_bits of the group's scale.
 template <int KIND>
-__device__ __forceinline__ uint4 w4_expand(uint32_t w, float scale) {
-  uint4 r;
+__device__ __forceinline__ u32x4 w4_expand(uint32_t w, float scale) {
+  u32x4 r;
   if constexpr (KIND == kMx) {
     r.x = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
     r.y = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
@@ -83,6 +85,10 @@ __device__ __forceinline__ uint4 w4_expand(uint32_t w, float scale) {
   }
   return r;
 }
+
+// The scale of an E2M1 group as the conversions take it: they read the exponent field alone, 0 as 2^-127
+// and 255 as NaN.
+__device__ __forceinline__ float mx_bits(uint32_t x) { return __uint_as_float(x << 23); }
 
 // The scale of an E2M1 group: 2^(x - 127), x = 0 the subnormal 2^-127, x = 255 NaN.
 __device__ __forceinline__ float mx_scale(uint32_t x) {
