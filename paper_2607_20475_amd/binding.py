@@ -144,6 +144,11 @@ def _stream():
     return _raw_stream(torch.cuda.current_device())
 
 
+def _raw(dev):
+    """The current stream of device `dev`, the current one."""
+    return _stream() if _raw_stream is None else _raw_stream(dev)
+
+
 def _dtype_code(t):
     if t.dtype == torch.bfloat16:
         return BF16
@@ -459,35 +464,59 @@ def process_logits(logits, params, k_max, out_logits=None, out_probs=None, flags
 # ---------------------------------------------------------------------------
 # The two ends of the vocabulary: hidden states to logits, tokens to hidden states
 # ---------------------------------------------------------------------------
-def _rows(t, name, rows=None, cols=None, dtype=None, device=None):
-    """Checks a matrix whose rows are evenly strided and whose columns follow one another."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        raise SSError(f"{name} must be a matrix of rows with unit column stride")
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        raise SSError(f"{name} must be [{rows}, {cols}], got {list(t.shape)}")
-    if dtype is not None and t.dtype != dtype:
-        raise SSError(f"{name} must be {dtype}, got {t.dtype}")
-    _here(t, name, device)
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
-def _here(t, name, device=None):
+def _rows(t, name, dev, rows=None, cols=None, dtype=None):
+    """(row stride, type) of a matrix on device `dev` whose rows are evenly strided, apart, and whose columns
+    follow one another."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2:
+        raise SSError(f"{name} must be a matrix, got {list(shape)}")
+    R, n = shape
+    ld = stride[0]
+    if (n > 1 and stride[1] != 1) or (R > 1 and ld < n):
+        raise SSError(f"{name} must have rows with unit column stride")
+    if (rows is not None and R != rows) or (cols is not None and n != cols):
+        raise SSError(f"{name} must be [{'any' if rows is None else rows}, {'any' if cols is None else cols}], got {list(shape)}")
+    dt = _TYPES.get(t.dtype)
+    if dt is None or (dtype is not None and t.dtype != dtype):
+        raise SSError(f"{name} must be {dtype or 'bfloat16 or float32'}, got {t.dtype}")
+    if t.get_device() != dev:
+        _elsewhere(t, name)
+    return (ld if R > 1 or ld > n else n), dt
+
+
+def _elsewhere(t, name):
     """Calls go to the current device's current stream: what they read has to be there."""
-    if not t.is_cuda:
-        raise SSError(f"{name} is not on a GPU")
-    if t.device.index != torch.cuda.current_device() or (device is not None and t.device != device):
-        raise SSError(f"{name} is not on the current device")
+    raise SSError(f"{name} is not on a GPU" if not t.is_cuda else f"{name} is not on the current device")
 
 
-def _ld(t):
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-
-
-def _tokens(tokens):
+def _tokens(tokens, dev):
     if tokens.dim() != 1 or tokens.dtype != torch.int32 or not tokens.is_contiguous():
         raise SSError("tokens must be contiguous int32 [T]")
-    _here(tokens, "tokens")
+    if tokens.get_device() != dev:
+        _elsewhere(tokens, "tokens")
     return tokens.shape[0]
 
+
+def _table(table, dev):
+    if table.codes.get_device() != dev:
+        _elsewhere(table.codes, "table")
+
+
+def _space(ws, dev):
+    """(pointer, bytes) of a workspace."""
+    if ws.get_device() != dev:
+        _elsewhere(ws, "ws")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _device():
+    try:
+        return torch.cuda.current_device()
+    except RuntimeError:  # no GPU: every check of a tensor's place fails
+        return -2
 
 
 class W4:
@@ -533,17 +562,13 @@ class W4:
 def quantize_w4(w, table=None, fmt="int", group=128, values=None):
     """The 4-bit form of w [V, H] (bfloat16 or float32), written to ``table`` (a new one of ``fmt`` and ``group`` if
     None) and returned; ``values`` [V, H], if given, gets the numbers that the codes stand for."""
-    _rows(w, "w")
+    dev = _device()
+    ld, dt = _rows(w, "w", dev, *(() if table is None else (table.V, table.H)))
     if table is None:
         table = W4.empty(w.shape[0], w.shape[1], fmt, group, w.device)
-    if w.shape != (table.V, table.H):
-        raise SSError(f"w must be [{table.V}, {table.H}], got {list(w.shape)}")
-    _here(table.codes, "table")
-    if values is not None:
-        _rows(values, "values", table.V, table.H)
-    _check(lib().ss_quant_w4(_ptr(w), _dtype_code(w), _ld(w), table._ref, _ptr(values),
-                             F32 if values is None else _dtype_code(values), 0 if values is None else _ld(values),
-                             _stream()))
+    _table(table, dev)
+    vld, vdt = (0, F32) if values is None else _rows(values, "values", dev, table.V, table.H)
+    _check(lib().ss_quant_w4(w.data_ptr(), dt, ld, table._ref, _ptr(values), vdt, vld, _raw(dev)))
     return table
 
 
@@ -557,41 +582,40 @@ def head_workspace(h):
 
 def head_w4(h, table, out=None, dtype=None, ws=None):
     """Logits [T, V] of hidden states h [T, H] under a 4-bit table; ``dtype`` (of a new ``out``): that of h."""
-    _rows(h, "h", cols=table.H)
-    _here(table.codes, "table")
+    dev = _device()
+    ld, dt = _rows(h, "h", dev, None, table.H)
+    _table(table, dev)
     T = h.shape[0]
     if out is None:
         out = torch.empty(T, table.V, dtype=dtype or h.dtype, device=h.device)
-    else:
-        _rows(out, "out", T, table.V, dtype)
+    old, odt = _rows(out, "out", dev, T, table.V, dtype)
     if ws is None:
         ws = head_workspace(h)
-    _here(ws, "ws")
-    _check(lib().ss_head_w4(_ptr(h), _dtype_code(h), T, _ld(h), table._ref, _ptr(out), _dtype_code(out), _ld(out),
-                            _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    space, n = _space(ws, dev)
+    _check(lib().ss_head_w4(h.data_ptr(), dt, T, ld, table._ref, out.data_ptr(), odt, old, space, n, _raw(dev)))
     return out
 
 
 def embed(tokens, table, scale=1.0, out=None, dtype=None):
     """scale * table[tokens] for int32 tokens [T] and a table [V, H] (a matrix or a ``W4``); tokens outside
     [0, V) give rows of zeros.  ``dtype`` (of a new ``out``): the matrix's, bfloat16 for a ``W4``."""
-    T = _tokens(tokens)
+    dev = _device()
+    T = _tokens(tokens, dev)
     w4 = isinstance(table, W4)
     if w4:
-        V, H = table.V, table.H
-        _here(table.codes, "table")
+        H = table.H
+        _table(table, dev)
     else:
-        _rows(table, "table")
+        ld, dt = _rows(table, "table", dev)
         V, H = table.shape
     if out is None:
         out = torch.empty(T, H, dtype=dtype or (torch.bfloat16 if w4 else table.dtype), device=tokens.device)
-    else:
-        _rows(out, "out", T, H, dtype)
+    old, odt = _rows(out, "out", dev, T, H, dtype)
     if w4:
-        st = lib().ss_embed_w4(_ptr(tokens), T, table._ref, scale, _ptr(out), _dtype_code(out), _ld(out), _stream())
+        st = lib().ss_embed_w4(tokens.data_ptr(), T, table._ref, scale, out.data_ptr(), odt, old, _raw(dev))
     else:
-        st = lib().ss_embed(_ptr(tokens), T, _ptr(table), _dtype_code(table), V, H, _ld(table), scale, _ptr(out),
-                            _dtype_code(out), _ld(out), _stream())
+        st = lib().ss_embed(tokens.data_ptr(), T, table.data_ptr(), dt, V, H, ld, scale, out.data_ptr(), odt, old,
+                            _raw(dev))
     _check(st)
     return out
 
@@ -607,22 +631,21 @@ def embed_grad_workspace(T, V, H, device="cuda"):
 def embed_grad(dout, tokens, V, scale=1.0, out=None, dtype=torch.float32, accumulate=False, ws=None):
     """The table's gradient [V, H] of ``embed``: scale * the sum of dout [T, H] over each token's positions.
     ``accumulate`` adds it to ``out`` and leaves the rows that no token names as they were."""
-    _rows(dout, "dout")
+    dev = _device()
+    ld, dt = _rows(dout, "dout", dev)
     T, H = dout.shape
-    if _tokens(tokens) != T:
+    if _tokens(tokens, dev) != T:
         raise SSError("tokens and dout must have as many rows")
     if out is None:
         if accumulate:
             raise SSError("accumulate needs out")
         out = torch.empty(V, H, dtype=dtype, device=dout.device)
-    else:
-        _rows(out, "out", V, H)
+    old, odt = _rows(out, "out", dev, V, H)
     if ws is None:
         ws = embed_grad_workspace(T, V, H, dout.device)
-    _here(ws, "ws")
-    _check(lib().ss_embed_grad(_ptr(dout), _dtype_code(dout), T, _ld(dout), _ptr(tokens), V, H, scale, _ptr(out),
-                               _dtype_code(out), _ld(out), accumulate, _ptr(ws), ws.numel() * ws.element_size(),
-                               _stream()))
+    space, n = _space(ws, dev)
+    _check(lib().ss_embed_grad(dout.data_ptr(), dt, T, ld, tokens.data_ptr(), V, H, scale, out.data_ptr(), odt, old,
+                               accumulate, space, n, _raw(dev)))
     return out
 
 
