@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void ss_embed_w4_kernel(EmbedArgs a) {
 constexpr int kRange = 256;      // ids of a sorting workgroup
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kRun = 128;        // longest run that its row adds by itself
+constexpr int kRun = 64;         // longest run that its row adds by itself
 
 struct GradArgs {
   const void* dout;
@@ -115,11 +115,24 @@ __global__ __launch_bounds__(kSortThreads) void ss_grad_sort_kernel(GradArgs a) 
   const int end = s0 + stretch < a.T ? (int)(s0 + stretch) : a.T;
   for (int i = tid; i < kSortWaves * kRange; i += kSortThreads) (&place[0][0])[i] = 0;
   __syncthreads();
+  constexpr int BATCH = 8;  // 64s of tokens in flight
+  auto load = [&](int t0, int (&v)[BATCH]) {
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const int t = t0 + i * 64 + lane;
+      const int x = a.tokens[t < end ? t : end - 1];
+      v[i] = t < end ? x : -1;
+    }
+  };
   int under = 0;
-  for (int t = begin + lane; t < end; t += 64) {
-    const int v = a.tokens[t];
-    under += v >= 0 && v < v0;
-    if (v >= v0 && v < v1) atomicAdd(&place[wave][v - v0], 1);
+  for (int t0 = begin; t0 < end; t0 += 64 * BATCH) {
+    int v[BATCH];
+    load(t0, v);
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      under += v[i] >= 0 && v[i] < v0;
+      if (v[i] >= v0 && v[i] < v1) atomicAdd(&place[wave][v[i] - v0], 1);
+    }
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) under += __shfl_xor(under, d);
@@ -151,24 +164,28 @@ __global__ __launch_bounds__(kSortThreads) void ss_grad_sort_kernel(GradArgs a) 
   }
   __syncthreads();
   volatile int* mp = place[wave];
-  for (int t0 = begin; t0 < end; t0 += 64) {
-    const int t = t0 + lane;
-    const int v = t < end ? a.tokens[t] : -1;
-    const bool in = v >= v0 && v < v1;
-    uint64_t same = __ballot(in);
-    if (!same) continue;
-    const int id = in ? v - v0 : 0;
+  for (int t0 = begin; t0 < end; t0 += 64 * BATCH) {
+    int batch[BATCH];
+    load(t0, batch);
 #pragma unroll
-    for (int bit = 1; bit < kRange; bit <<= 1) {
-      const uint64_t b = __ballot(in && (id & bit));
-      same &= (id & bit) ? b : ~b;
-    }
-    if (in) {  // lanes of one id: places in lane order, the last lane moves the id on
-      const int rank = __popcll(same & ((1ull << lane) - 1ull));
-      const int at = mp[id] + rank;
-      a.perm[at] = t;
-      a.ids[at] = v;
-      if (rank + 1 == __popcll(same)) mp[id] = at + 1;
+    for (int i = 0; i < BATCH; ++i) {
+      const int v = batch[i];
+      const bool in = v >= v0 && v < v1;
+      uint64_t same = __ballot(in);
+      if (!same) continue;
+      const int id = in ? v - v0 : 0;
+#pragma unroll
+      for (int bit = 1; bit < kRange; bit <<= 1) {
+        const uint64_t b = __ballot(in && (id & bit));
+        same &= (id & bit) ? b : ~b;
+      }
+      if (in) {  // lanes of one id: places in lane order, the last lane moves the id on
+        const int rank = __popcll(same & ((1ull << lane) - 1ull));
+        const int at = mp[id] + rank;
+        a.perm[at] = t0 + i * 64 + lane;
+        a.ids[at] = v;
+        if (rank + 1 == __popcll(same)) mp[id] = at + 1;
+      }
     }
   }
 }
@@ -176,85 +193,174 @@ __global__ __launch_bounds__(kSortThreads) void ss_grad_sort_kernel(GradArgs a) 
 // ---------------------------------------------------------------------------
 // Gradient: sums
 // ---------------------------------------------------------------------------
-// Adds list entries [p0, p1) of eight columns, in order, four rows in flight.
-template <int DT>
-__device__ __forceinline__ void add_rows(const GradArgs& a, int p0, int p1, int col, float x[8]) {
-  const int left = a.H - col;
-  int p = p0;
-  for (; p + 4 <= p1; p += 4) {
-    float y[4][8];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) row_load8<DT>(a.dout, (int64_t)a.perm[p + q] * a.ld + col, left, a.wide_in, y[q]);
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] += y[q][i];
+// A thread's columns of a tile of kCols: one octet where the table is bfloat16, two quads half a tile apart where it is
+// float32, so that a wave's loads and stores are up to 16 bytes a lane and lie together.
+template <int ODT>
+struct Cols {
+  static constexpr int kPieces = ODT == SS_F32 ? 2 : 1, kWide = 8 / kPieces;
+  static __device__ int at(int piece) {
+    return blockIdx.y * kCols + piece * (kCols / kPieces) + (int)threadIdx.x * kWide;
   }
-  for (; p < p1; ++p) {
+};
+
+// N columns of a row in float32, `left` of which it has.
+template <int DT, int N>
+__device__ __forceinline__ void cols_load(const void* p, int64_t at, int left, bool wide, float* x) {
+  if constexpr (N == 8) {
     float y[8];
-    row_load8<DT>(a.dout, (int64_t)a.perm[p] * a.ld + col, left, a.wide_in, y);
+    row_load8<DT>(p, at, left, wide, y);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] += y[i];
+    for (int i = 0; i < 8; ++i) x[i] = y[i];
+  } else if (wide && left >= 4) {
+    if constexpr (DT == SS_F32) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(p) + at);
+      x[0] = v[0], x[1] = v[1], x[2] = v[2], x[3] = v[3];
+    } else {
+      const uint2 u = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(p) + at);
+      x[0] = __uint_as_float(u.x << 16), x[1] = __uint_as_float(u.x & 0xFFFF0000u);
+      x[2] = __uint_as_float(u.y << 16), x[3] = __uint_as_float(u.y & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = 0.0f;
+      if (i < left)
+        x[i] = DT == SS_F32 ? reinterpret_cast<const float*>(p)[at + i] : bf16_value(reinterpret_cast<const uint16_t*>(p)[at + i]);
+    }
   }
 }
 
-__device__ __forceinline__ void put_part(const GradArgs& a, int cut, int piece, int col, const float x[8]) {
-  float* o = a.part + ((int64_t)cut * 2 + piece) * a.H + col;
+template <int DT, int N>
+__device__ __forceinline__ void cols_store(void* p, int64_t at, int left, bool wide, const float* x) {
+  if constexpr (N == 8) {
+    float y[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (col + i < a.H) o[i] = x[i];
+    for (int i = 0; i < 8; ++i) y[i] = x[i];
+    row_store8<DT>(p, at, left, wide, y);
+  } else if (wide && left >= 4) {
+    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(p) + at) = f32x4{x[0], x[1], x[2], x[3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < left) reinterpret_cast<float*>(p)[at + i] = x[i];
+  }
+}
+
+// Adds list entries [p0, p1) of a thread's columns, in order, kDeep rows in flight.
+constexpr int kDeep = 8;
+template <int DT, int ODT>
+__device__ __forceinline__ void add_rows(const GradArgs& a, int p0, int p1, float x[8]) {
+  using C = Cols<ODT>;
+  for (int p = p0; p < p1; p += kDeep) {
+    float y[kDeep][8];
+#pragma unroll
+    for (int q = 0; q < kDeep; ++q) {
+      if (p + q < p1) {
+        const int64_t row = (int64_t)a.perm[p + q] * a.ld;
+#pragma unroll
+        for (int i = 0; i < C::kPieces; ++i)
+          cols_load<DT, C::kWide>(a.dout, row + C::at(i), a.H - C::at(i), a.wide_in, y[q] + i * C::kWide);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kDeep; ++q) {
+      if (p + q < p1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] += y[q][i];
+      }
+    }
+  }
+}
+
+// Piece `piece` of a cut's two parts, float32 rows of H columns rounded up to 4.
+template <int ODT>
+__device__ __forceinline__ float* part_row(const GradArgs& a, int cut, int piece) {
+  return a.part + ((int64_t)cut * 2 + piece) * ((a.H + 3) & ~3);
+}
+
+template <int DT, int ODT>
+__device__ __forceinline__ void sum_part(const GradArgs& a, int p0, int p1, int cut, int piece) {
+  using C = Cols<ODT>;
+  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  add_rows<DT, ODT>(a, p0, p1, x);
+  float* o = part_row<ODT>(a, cut, piece);
+#pragma unroll
+  for (int i = 0; i < 8; i += 4) {
+    const int col = C::at(i / C::kWide) + i % C::kWide;
+    if (col < a.H) cols_store<SS_F32, 4>(o, col, 4, true, x + i);
+  }
 }
 
 // A cut of kRun entries holds parts of two long runs at most: one that began at or before
 // its first entry (piece 0) and one that begins later and leaves it (piece 1).
-template <int DT>
+template <int DT, int ODT>
 __global__ __launch_bounds__(256) void ss_grad_parts_kernel(GradArgs a) {
-  const int cut = blockIdx.x, col = blockIdx.y * kCols + threadIdx.x * 8;
+  const int cut = blockIdx.x;
   const int n = a.start[a.V];
   const int p0 = cut * kRun, p1 = p0 + kRun < n ? p0 + kRun : n;
-  if (p0 >= p1 || col >= a.H) return;
+  if (p0 >= p1) return;
   const int u = a.ids[p0], u0 = a.start[u], u1 = a.start[u + 1];
   const int w = a.ids[p1 - 1], w0 = a.start[w], w1 = a.start[w + 1];
-  if (u1 - u0 > kRun) {
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    add_rows<DT>(a, p0, u1 < p1 ? u1 : p1, col, x);
-    put_part(a, cut, 0, col, x);
-  }
-  if (w != u && w1 - w0 > kRun) {
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    add_rows<DT>(a, w0, p1, col, x);
-    put_part(a, cut, 1, col, x);
-  }
+  if (u1 - u0 > kRun) sum_part<DT, ODT>(a, p0, u1 < p1 ? u1 : p1, cut, 0);
+  if (w != u && w1 - w0 > kRun) sum_part<DT, ODT>(a, w0, p1, cut, 1);
 }
+
+constexpr int kRows = 8;  // of a workgroup: what it takes to start one is spread over them
 
 template <int DT, int ODT>
 __global__ __launch_bounds__(256) void ss_grad_rows_kernel(GradArgs a) {
-  const int v = blockIdx.x;
-  const int col = blockIdx.y * kCols + threadIdx.x * 8;
-  if (col >= a.H) return;
-  const int p0 = a.start[v], p1 = a.start[v + 1];
-  if (a.accumulate && p0 == p1) return;
-  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (p1 - p0 <= kRun) {
-    add_rows<DT>(a, p0, p1, col, x);
-  } else {
-    for (int cut = p0 / kRun; cut * kRun < p1; ++cut) {
-      const float* q = a.part + ((int64_t)cut * 2 + (p0 > cut * kRun)) * a.H + col;
+  using C = Cols<ODT>;
+  const int v0 = blockIdx.x * kRows;
+  int start[kRows + 1];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (col + i < a.H) x[i] += q[i];
+  for (int r = 0; r <= kRows; ++r) start[r] = a.start[v0 + r < a.V ? v0 + r : a.V];
+  if (!a.accumulate) {
+    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      if (start[r] != start[r + 1] || v0 + r >= a.V) continue;
+#pragma unroll
+      for (int i = 0; i < C::kPieces; ++i)
+        cols_store<ODT, C::kWide>(a.out, (int64_t)(v0 + r) * a.ld_out + C::at(i), a.H - C::at(i), a.wide_out, zero);
     }
   }
-  const int64_t at = (int64_t)v * a.ld_out + col;
+#pragma unroll 1
+  for (int r = 0; r < kRows; ++r) {
+    const int v = v0 + r;
+    if (v >= a.V) break;
+    const int p0 = a.start[v], p1 = a.start[v + 1];
+    if (p0 == p1) continue;
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (p1 - p0 <= kRun) {
+      add_rows<DT, ODT>(a, p0, p1, x);
+    } else {
+      for (int cut = p0 / kRun; cut * kRun < p1; ++cut) {
+        const float* q = part_row<ODT>(a, cut, p0 > cut * kRun);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] *= a.scale;
-  if (a.accumulate) {
-    float y[8];
-    row_load8<ODT>(a.out, at, a.H - col, a.wide_out, y);
+        for (int i = 0; i < 8; i += 4) {
+          const int col = C::at(i / C::kWide) + i % C::kWide;
+          float y[4] = {0.f, 0.f, 0.f, 0.f};
+          if (col < a.H) cols_load<SS_F32, 4>(q, col, 4, true, y);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] += y[i];
+          for (int k = 0; k < 4; ++k) x[i + k] += y[k];
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= a.scale;
+#pragma unroll
+    for (int i = 0; i < C::kPieces; ++i) {
+      const int64_t at = (int64_t)v * a.ld_out + C::at(i);
+      const int left = a.H - C::at(i);
+      if (a.accumulate) {
+        float y[8];
+        cols_load<ODT, C::kWide>(a.out, at, left, a.wide_out, y);
+#pragma unroll
+        for (int k = 0; k < C::kWide; ++k) x[i * C::kWide + k] += y[k];
+      }
+      cols_store<ODT, C::kWide>(a.out, at, left, a.wide_out, x + i * C::kWide);
+    }
   }
-  row_store8<ODT>(a.out, at, a.H - col, a.wide_out, x);
 }
 
 // ---------------------------------------------------------------------------
@@ -272,9 +378,19 @@ static bool grad_layout(int T, int V, int H, GradLayout* l) {
   l->start = o, o = align256(o + ((size_t)V + 1) * 4);
   l->perm = o, o = align256(o + (size_t)T * 4);
   l->ids = o, o = align256(o + (size_t)T * 4);
-  l->part = o, o = align256(o + (size_t)((T + kRun - 1) / kRun) * 2 * H * 4);
+  l->part = o, o = align256(o + (size_t)((T + kRun - 1) / kRun) * 2 * ((H + 3) & ~3) * 4);
   l->total = o;
   return true;
+}
+
+template <int DT, int ODT>
+static void launch_sums(const GradArgs& a, unsigned tiles, hipStream_t st) {
+  if (a.T > kRun) {
+    const dim3 grid((unsigned)((a.T + kRun - 1) / kRun), tiles);
+    hipLaunchKernelGGL((ss_grad_parts_kernel<DT, ODT>), grid, dim3(256), 0, st, a);
+  }
+  const dim3 grid((unsigned)((a.V + kRows - 1) / kRows), tiles);
+  hipLaunchKernelGGL((ss_grad_rows_kernel<DT, ODT>), grid, dim3(256), 0, st, a);
 }
 
 template <int KIND>
@@ -385,22 +501,10 @@ ss_status ss_embed_grad(const void* dout, int dtype, int T, int64_t ld, const in
   const hipStream_t st = (hipStream_t)stream;
   const unsigned tiles = (unsigned)((H + kCols - 1) / kCols);
   hipLaunchKernelGGL(ss_grad_sort_kernel, dim3((unsigned)((V + kRange - 1) / kRange)), dim3(kSortThreads), 0, st, a);
-  if (T > kRun) {
-    const dim3 grid((unsigned)((T + kRun - 1) / kRun), tiles);
-    if (dtype == SS_F32)
-      hipLaunchKernelGGL(ss_grad_parts_kernel<SS_F32>, grid, dim3(256), 0, st, a);
-    else
-      hipLaunchKernelGGL(ss_grad_parts_kernel<SS_BF16>, grid, dim3(256), 0, st, a);
-  }
-  const dim3 grid((unsigned)V, tiles);
-  if (dtype == SS_F32 && out_dtype == SS_F32)
-    hipLaunchKernelGGL((ss_grad_rows_kernel<SS_F32, SS_F32>), grid, dim3(256), 0, st, a);
-  else if (dtype == SS_F32)
-    hipLaunchKernelGGL((ss_grad_rows_kernel<SS_F32, SS_BF16>), grid, dim3(256), 0, st, a);
-  else if (out_dtype == SS_F32)
-    hipLaunchKernelGGL((ss_grad_rows_kernel<SS_BF16, SS_F32>), grid, dim3(256), 0, st, a);
+  if (dtype == SS_F32)
+    out_dtype == SS_F32 ? launch_sums<SS_F32, SS_F32>(a, tiles, st) : launch_sums<SS_F32, SS_BF16>(a, tiles, st);
   else
-    hipLaunchKernelGGL((ss_grad_rows_kernel<SS_BF16, SS_BF16>), grid, dim3(256), 0, st, a);
+    out_dtype == SS_F32 ? launch_sums<SS_BF16, SS_F32>(a, tiles, st) : launch_sums<SS_BF16, SS_BF16>(a, tiles, st);
   return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_HIP;
 }
 
