@@ -85,25 +85,27 @@ __global__ __launch_bounds__(256) void ss_embed_w4_kernel(EmbedArgs a) {
 constexpr int kRange = 256;      // ids of a sorting workgroup
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kRun = 64;         // longest run that its row adds by itself
+constexpr int kFewLanes = 8;
+constexpr int kRun = 32;         // longest run that its row adds by itself
 
 struct GradArgs {
   const void* dout;
   const int32_t* tokens;
   void* out;
   int32_t* start;   // [V + 1] first place of each id in the list
-  int32_t* perm;    // [T] positions, by id and position
-  int32_t* ids;     // [T] ids of the list
+  int4* list;       // [T] by id and position: the position, the id, its run's first and last place + 1
   float* part;      // [cuts][2][H] sums of long runs' parts
   int64_t ld, ld_out;
   float scale;
   int T, V, H;
   int wide_in, wide_out, accumulate;
+  uint32_t tiles, wtiles, cuts, heads;  // column tiles, one and kWide; cuts of the list; groups of kHeads entries
 };
 
 __global__ __launch_bounds__(kSortThreads) void ss_grad_sort_kernel(GradArgs a) {
   __shared__ int place[kSortWaves][kRange];
-  __shared__ int total[kRange];
+  __shared__ int run[kRange][2];
+  __shared__ int total[kRange / 64];
   __shared__ int below[kSortWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int v0 = blockIdx.x * kRange;
@@ -115,58 +117,61 @@ __global__ __launch_bounds__(kSortThreads) void ss_grad_sort_kernel(GradArgs a) 
   const int end = s0 + stretch < a.T ? (int)(s0 + stretch) : a.T;
   for (int i = tid; i < kSortWaves * kRange; i += kSortThreads) (&place[0][0])[i] = 0;
   __syncthreads();
-  constexpr int BATCH = 8;  // 64s of tokens in flight
-  auto load = [&](int t0, int (&v)[BATCH]) {
+  constexpr int BATCH = 16;  // 64s of tokens in flight
+  int batch[BATCH];
+  auto load = [&](int t0) {
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
       const int t = t0 + i * 64 + lane;
       const int x = a.tokens[t < end ? t : end - 1];
-      v[i] = t < end ? x : -1;
+      batch[i] = t < end ? x : -1;
     }
   };
   int under = 0;
   for (int t0 = begin; t0 < end; t0 += 64 * BATCH) {
-    int v[BATCH];
-    load(t0, v);
+    load(t0);
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
-      under += v[i] >= 0 && v[i] < v0;
-      if (v[i] >= v0 && v[i] < v1) atomicAdd(&place[wave][v[i] - v0], 1);
+      under += batch[i] >= 0 && batch[i] < v0;
+      if (batch[i] >= v0 && batch[i] < v1) atomicAdd(&place[wave][batch[i] - v0], 1);
     }
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) under += __shfl_xor(under, d);
   if (lane == 0) below[wave] = under;
   __syncthreads();
-  int mine = 0;  // of id v0 + tid: its places, and each wave's first among them
+  int mine = 0, upto = 0;  // of id v0 + tid: its places; of it and its wave's ids before it
   if (tid < kRange) {
-    for (int w = 0; w < kSortWaves; ++w) {
-      const int c = place[w][tid];
-      place[w][tid] = mine;
-      mine += c;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) mine += place[w][tid];
+    upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(upto, d);
+      if (lane >= d) upto += o;
     }
-    total[tid] = mine;
+    if (lane == 63) total[wave] = upto;
   }
   __syncthreads();
-  for (int d = 1; d < kRange; d <<= 1) {  // inclusive sums over the range
-    int add = 0;
-    if (tid < kRange && tid >= d) add = total[tid - d];
-    __syncthreads();
-    if (tid < kRange) total[tid] += add;
-    __syncthreads();
-  }
   if (tid < kRange) {
-    int first = total[tid] - mine;
+    int first = upto - mine;
+    for (int w = 0; w < wave; ++w) first += total[w];
+#pragma unroll
     for (int w = 0; w < kSortWaves; ++w) first += below[w];
     if (v0 + tid < a.V) a.start[v0 + tid] = first;
     if (v0 + tid == a.V - 1) a.start[a.V] = first + mine;
-    for (int w = 0; w < kSortWaves; ++w) place[w][tid] += first;
+    run[tid][0] = first, run[tid][1] = first + mine;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {  // each wave's first place of the id
+      const int c = place[w][tid];
+      place[w][tid] = first;
+      first += c;
+    }
   }
   __syncthreads();
   volatile int* mp = place[wave];
   for (int t0 = begin; t0 < end; t0 += 64 * BATCH) {
-    int batch[BATCH];
-    load(t0, batch);
+    if (end - begin > 64 * BATCH) load(t0);  // else the first scan's are still there
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
       const int v = batch[i];
@@ -174,16 +179,25 @@ __global__ __launch_bounds__(kSortThreads) void ss_grad_sort_kernel(GradArgs a) 
       uint64_t same = __ballot(in);
       if (!same) continue;
       const int id = in ? v - v0 : 0;
+      // the lanes of each lane's id: few lanes id by id, many bit by bit
+      if (__popcll(same) <= kFewLanes) {
+        for (uint64_t todo = same; todo;) {
+          const int one = __builtin_amdgcn_readlane(id, __ffsll((unsigned long long)todo) - 1);
+          const uint64_t m = __ballot(in && id == one);
+          if (id == one) same = m;
+          todo &= ~m;
+        }
+      } else {
 #pragma unroll
-      for (int bit = 1; bit < kRange; bit <<= 1) {
-        const uint64_t b = __ballot(in && (id & bit));
-        same &= (id & bit) ? b : ~b;
+        for (int bit = 1; bit < kRange; bit <<= 1) {
+          const uint64_t b = __ballot(in && (id & bit));
+          same &= (id & bit) ? b : ~b;
+        }
       }
       if (in) {  // lanes of one id: places in lane order, the last lane moves the id on
         const int rank = __popcll(same & ((1ull << lane) - 1ull));
         const int at = mp[id] + rank;
-        a.perm[at] = t0 + i * 64 + lane;
-        a.ids[at] = v;
+        a.list[at] = make_int4(t0 + i * 64 + lane, v, run[id][0], run[id][1]);
         if (rank + 1 == __popcll(same)) mp[id] = at + 1;
       }
     }
@@ -193,14 +207,10 @@ __global__ __launch_bounds__(kSortThreads) void ss_grad_sort_kernel(GradArgs a) 
 // ---------------------------------------------------------------------------
 // Gradient: sums
 // ---------------------------------------------------------------------------
-// A thread's columns of a tile of kCols: one octet where the table is bfloat16, two quads half a tile apart where it is
-// float32, so that a wave's loads and stores are up to 16 bytes a lane and lie together.
+// A thread has 16 bytes of the table: N = 4 columns of float32 or 8 of bfloat16, of a tile of 256 N.
 template <int ODT>
 struct Cols {
-  static constexpr int kPieces = ODT == SS_F32 ? 2 : 1, kWide = 8 / kPieces;
-  static __device__ int at(int piece) {
-    return blockIdx.y * kCols + piece * (kCols / kPieces) + (int)threadIdx.x * kWide;
-  }
+  static constexpr int N = ODT == SS_F32 ? 4 : 8, kTile = 256 * N;
 };
 
 // N columns of a row in float32, `left` of which it has.
@@ -246,121 +256,176 @@ __device__ __forceinline__ void cols_store(void* p, int64_t at, int left, bool w
   }
 }
 
-// Adds list entries [p0, p1) of a thread's columns, in order, kDeep rows in flight.
-constexpr int kDeep = 8;
-template <int DT, int ODT>
-__device__ __forceinline__ void add_rows(const GradArgs& a, int p0, int p1, float x[8]) {
-  using C = Cols<ODT>;
-  for (int p = p0; p < p1; p += kDeep) {
-    float y[kDeep][8];
+// Adds D list entries from p on, all in flight at once: W pieces of N columns, a tile apart, from col on.
+template <int DT, int N, int W, int D>
+__device__ __forceinline__ void add_some(const GradArgs& a, int p, int col, float (&x)[W][N]) {
+  int t[D];
+  float y[D][W][N];
 #pragma unroll
-    for (int q = 0; q < kDeep; ++q) {
-      if (p + q < p1) {
-        const int64_t row = (int64_t)a.perm[p + q] * a.ld;
+  for (int q = 0; q < D; ++q) t[q] = a.list[p + q].x;
 #pragma unroll
-        for (int i = 0; i < C::kPieces; ++i)
-          cols_load<DT, C::kWide>(a.dout, row + C::at(i), a.H - C::at(i), a.wide_in, y[q] + i * C::kWide);
-      }
+  for (int q = 0; q < D; ++q)
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const int c = col + w * 256 * N;
+      cols_load<DT, N>(a.dout, (int64_t)t[q] * a.ld + c, a.H - c, a.wide_in, y[q][w]);
     }
 #pragma unroll
-    for (int q = 0; q < kDeep; ++q) {
-      if (p + q < p1) {
+  for (int q = 0; q < D; ++q)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] += y[q][i];
-      }
-    }
-  }
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[w][i] += y[q][w][i];
 }
 
-// Piece `piece` of a cut's two parts, float32 rows of H columns rounded up to 4.
-template <int ODT>
+// Adds list entries [p0, p1), in order.
+template <int DT, int N, int W>
+__device__ __forceinline__ void add_rows(const GradArgs& a, int p0, int p1, int col, float (&x)[W][N]) {
+  constexpr int D = (W == 1 ? 64 : 16) / N;
+#pragma unroll
+  for (int w = 0; w < W; ++w)
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[w][i] = 0.0f;
+  int p = p0;
+  for (; p + D <= p1; p += D) add_some<DT, N, W, D>(a, p, col, x);
+  if constexpr (D > 8)
+    if (p + 8 <= p1) add_some<DT, N, W, 8>(a, p, col, x), p += 8;
+  if constexpr (D > 4)
+    if (p + 4 <= p1) add_some<DT, N, W, 4>(a, p, col, x), p += 4;
+  if constexpr (D > 2)
+    if (p + 2 <= p1) add_some<DT, N, W, 2>(a, p, col, x), p += 2;
+  if (p < p1) add_some<DT, N, W, 1>(a, p, col, x);
+}
+
+// Writes a row's sum, scaled and rounded, or adds it to the row.
+template <int ODT, int N>
+__device__ __forceinline__ void put_row(const GradArgs& a, int v, int col, float x[N]) {
+  const int64_t at = (int64_t)v * a.ld_out + col;
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] *= a.scale;
+  if (a.accumulate) {
+    float y[N];
+    cols_load<ODT, N>(a.out, at, a.H - col, a.wide_out, y);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += y[i];
+  }
+  cols_store<ODT, N>(a.out, at, a.H - col, a.wide_out, x);
+}
+
+// The two pieces of a cut, float32 rows of H columns rounded up to 8.
 __device__ __forceinline__ float* part_row(const GradArgs& a, int cut, int piece) {
-  return a.part + ((int64_t)cut * 2 + piece) * ((a.H + 3) & ~3);
+  return a.part + ((int64_t)cut * 2 + piece) * ((a.H + 7) & ~7);
 }
 
-template <int DT, int ODT>
-__device__ __forceinline__ void sum_part(const GradArgs& a, int p0, int p1, int cut, int piece) {
-  using C = Cols<ODT>;
-  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  add_rows<DT, ODT>(a, p0, p1, x);
-  float* o = part_row<ODT>(a, cut, piece);
-#pragma unroll
-  for (int i = 0; i < 8; i += 4) {
-    const int col = C::at(i / C::kWide) + i % C::kWide;
-    if (col < a.H) cols_store<SS_F32, 4>(o, col, 4, true, x + i);
-  }
+template <int DT, int N>
+__device__ __forceinline__ void sum_part(const GradArgs& a, int p0, int p1, int cut, int piece, int col) {
+  float x[1][N];
+  add_rows<DT, N, 1>(a, p0, p1, col, x);
+  cols_store<SS_F32, N>(part_row(a, cut, piece), col, N, true, x[0]);
 }
 
-// A cut of kRun entries holds parts of two long runs at most: one that began at or before
-// its first entry (piece 0) and one that begins later and leaves it (piece 1).
-template <int DT, int ODT>
-__global__ __launch_bounds__(256) void ss_grad_parts_kernel(GradArgs a) {
-  const int cut = blockIdx.x;
-  const int n = a.start[a.V];
-  const int p0 = cut * kRun, p1 = p0 + kRun < n ? p0 + kRun : n;
-  if (p0 >= p1) return;
-  const int u = a.ids[p0], u0 = a.start[u], u1 = a.start[u + 1];
-  const int w = a.ids[p1 - 1], w0 = a.start[w], w1 = a.start[w + 1];
-  if (u1 - u0 > kRun) sum_part<DT, ODT>(a, p0, u1 < p1 ? u1 : p1, cut, 0);
-  if (w != u && w1 - w0 > kRun) sum_part<DT, ODT>(a, w0, p1, cut, 1);
-}
-
-constexpr int kRows = 8;  // of a workgroup: what it takes to start one is spread over them
+// Three kinds of workgroups in one launch:
+//   parts   of long runs.  A cut of kRun entries holds parts of two such runs at most, one that began at or before
+//           its first entry (piece 0) and one that begins later and leaves it (piece 1).
+//   runs    the rows of the short runs that begin among kHeads entries.  The list, not the table, is
+//           shared out: wherever its rows lie, the runs go to all parts of the chip.
+//   zeros   the rows without a run, in the order of memory, kPieces pieces of 4 KB to a workgroup (none when accumulating).
+// The first two start first, the zeros' stores follow: dealt out in turn with them, loads and stores that lie apart slow
+// the stores in order down.  At 16384 tokens by Zipf's law, bfloat16 to float32, V = 131072, H = 4096 (2.27 GB): 452 us;
+// dealt out in turn 583; 1, 2, 4 and 8 pieces 642, 549, 538 and 587 (with the runs' rows among the zeros'); runs up to 16, 32 and
+// 64 entries short 456, 453 and 481; one entry a workgroup puts runs of equal lengths on few XCDs (2000 runs of 8: 648 against 464).
+constexpr int kHeads = 3, kPieces = 4, kWide = 2;
 
 template <int DT, int ODT>
 __global__ __launch_bounds__(256) void ss_grad_rows_kernel(GradArgs a) {
-  using C = Cols<ODT>;
-  const int v0 = blockIdx.x * kRows;
-  int start[kRows + 1];
-#pragma unroll
-  for (int r = 0; r <= kRows; ++r) start[r] = a.start[v0 + r < a.V ? v0 + r : a.V];
-  if (!a.accumulate) {
-    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      if (start[r] != start[r + 1] || v0 + r >= a.V) continue;
-#pragma unroll
-      for (int i = 0; i < C::kPieces; ++i)
-        cols_store<ODT, C::kWide>(a.out, (int64_t)(v0 + r) * a.ld_out + C::at(i), a.H - C::at(i), a.wide_out, zero);
-    }
+  constexpr int N = Cols<ODT>::N, TILE = Cols<ODT>::kTile;
+  uint32_t b = blockIdx.x + blockIdx.y * gridDim.x;
+  if (b < a.cuts * a.tiles) {
+    const int cut = (int)(b / a.tiles), col = (int)(b % a.tiles) * TILE + (int)threadIdx.x * N;
+    const int n = a.start[a.V];
+    const int p0 = cut * kRun, p1 = p0 + kRun < n ? p0 + kRun : n;
+    if (p0 >= p1 || col >= a.H) return;
+    const int4 u = a.list[p0], w = a.list[p1 - 1];
+    if (u.w - u.z > kRun) sum_part<DT, N>(a, p0, u.w < p1 ? u.w : p1, cut, 0, col);
+    if (w.y != u.y && w.w - w.z > kRun) sum_part<DT, N>(a, w.z, p1, cut, 1, col);
+    return;
   }
-#pragma unroll 1
-  for (int r = 0; r < kRows; ++r) {
-    const int v = v0 + r;
-    if (v >= a.V) break;
-    const int p0 = a.start[v], p1 = a.start[v + 1];
-    if (p0 == p1) continue;
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (p1 - p0 <= kRun) {
-      add_rows<DT, ODT>(a, p0, p1, x);
-    } else {
-      for (int cut = p0 / kRun; cut * kRun < p1; ++cut) {
-        const float* q = part_row<ODT>(a, cut, p0 > cut * kRun);
+  b -= a.cuts * a.tiles;
+  if (b < a.heads * a.wtiles) {
+    const int h = (int)(b / a.wtiles) * kHeads, col = (int)(b % a.wtiles) * (kWide * TILE) + (int)threadIdx.x * N;
+    const int n = a.start[a.V];
+    int4 e[kHeads];
 #pragma unroll
-        for (int i = 0; i < 8; i += 4) {
-          const int col = C::at(i / C::kWide) + i % C::kWide;
-          float y[4] = {0.f, 0.f, 0.f, 0.f};
-          if (col < a.H) cols_load<SS_F32, 4>(q, col, 4, true, y);
+    for (int k = 0; k < kHeads; ++k) e[k] = a.list[h + k < a.T ? h + k : a.T - 1];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) x[i + k] += y[k];
+    for (int k = 0; k < kHeads; ++k) {
+      // not in the list, not a run's first entry, or a long run's
+      if (h + k >= n || e[k].z != h + k || e[k].w - e[k].z > kRun) continue;
+      float x[kWide][N];
+      add_rows<DT, N, kWide>(a, e[k].z, e[k].w, col, x);
+#pragma unroll
+      for (int w = 0; w < kWide; ++w) put_row<ODT, N>(a, e[k].y, col + w * TILE, x[w]);
+    }
+    return;
+  }
+  b -= a.heads * a.wtiles;
+  const float zero[N] = {};
+  uint32_t v[kPieces];
+  bool none[kPieces];
+#pragma unroll
+  for (int k = 0; k < kPieces; ++k) {
+    v[k] = (b * kPieces + k) / a.tiles;
+    none[k] = v[k] < (uint32_t)a.V && a.start[v[k]] == a.start[v[k] + 1];
+  }
+#pragma unroll
+  for (int k = 0; k < kPieces; ++k) {
+    const int col = (int)(b * kPieces + k - v[k] * a.tiles) * TILE + (int)threadIdx.x * N;
+    if (none[k]) cols_store<ODT, N>(a.out, (int64_t)v[k] * a.ld_out + col, a.H - col, a.wide_out, zero);
+  }
+}
+
+// The rows of long runs: the workgroup of the cut that such a run begins in adds its parts; each wave a quarter of them,
+// in order, and the quarters in order.
+template <int ODT>
+__global__ __launch_bounds__(256) void ss_grad_join_kernel(GradArgs a) {
+  constexpr int N = Cols<ODT>::N, D = 64 / N;
+  __shared__ float sums[4][64][N];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int cut = blockIdx.x, col = blockIdx.y * (64 * N) + lane * N;
+  const int n = a.start[a.V];
+  const int p0 = cut * kRun, p1 = p0 + kRun < n ? p0 + kRun : n;
+  if (p0 >= p1) return;
+  const int4 e = a.list[p1 - 1];
+  if (e.z < p0 || e.w - e.z <= kRun) return;
+  float x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = 0.0f;
+  const int parts = (e.w - 1) / kRun + 1 - cut, from = parts * wave / 4, to = parts * (wave + 1) / 4;
+  if (col < a.H) {
+    for (int c = from; c < to; c += D) {
+      float y[D][N];
+#pragma unroll
+      for (int q = 0; q < D; ++q) {
+        const int k = c + q < to ? c + q : to - 1;
+        cols_load<SS_F32, N>(part_row(a, cut + k, k == 0 && e.z > p0), col, N, true, y[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < D; ++q)
+        if (c + q < to) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) x[i] += y[q][i];
         }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] *= a.scale;
-#pragma unroll
-    for (int i = 0; i < C::kPieces; ++i) {
-      const int64_t at = (int64_t)v * a.ld_out + C::at(i);
-      const int left = a.H - C::at(i);
-      if (a.accumulate) {
-        float y[8];
-        cols_load<ODT, C::kWide>(a.out, at, left, a.wide_out, y);
-#pragma unroll
-        for (int k = 0; k < C::kWide; ++k) x[i * C::kWide + k] += y[k];
-      }
-      cols_store<ODT, C::kWide>(a.out, at, left, a.wide_out, x + i * C::kWide);
     }
   }
+#pragma unroll
+  for (int i = 0; i < N; ++i) sums[wave][lane][i] = x[i];
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w)
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += sums[w][lane][i];
+  put_row<ODT, N>(a, e.y, col, x);
 }
 
 // ---------------------------------------------------------------------------
@@ -370,27 +435,31 @@ static bool is_type(int dt) { return dt == SS_F32 || dt == SS_BF16; }
 static size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 struct GradLayout {
-  size_t start, perm, ids, part, total;
+  size_t start, list, part, total;
 };
 static bool grad_layout(int T, int V, int H, GradLayout* l) {
   if (T < 0 || T > SS_MAX_T || V < 1 || V > SS_MAX_V || H < 1 || H > SS_MAX_H) return false;
   size_t o = 0;
   l->start = o, o = align256(o + ((size_t)V + 1) * 4);
-  l->perm = o, o = align256(o + (size_t)T * 4);
-  l->ids = o, o = align256(o + (size_t)T * 4);
-  l->part = o, o = align256(o + (size_t)((T + kRun - 1) / kRun) * 2 * ((H + 3) & ~3) * 4);
+  l->list = o, o = align256(o + (size_t)T * 16);
+  l->part = o, o = align256(o + (size_t)((T + kRun - 1) / kRun) * 2 * ((H + 7) & ~7) * 4);
   l->total = o;
   return true;
 }
 
 template <int DT, int ODT>
-static void launch_sums(const GradArgs& a, unsigned tiles, hipStream_t st) {
-  if (a.T > kRun) {
-    const dim3 grid((unsigned)((a.T + kRun - 1) / kRun), tiles);
-    hipLaunchKernelGGL((ss_grad_parts_kernel<DT, ODT>), grid, dim3(256), 0, st, a);
-  }
-  const dim3 grid((unsigned)((a.V + kRows - 1) / kRows), tiles);
+static void launch_sums(GradArgs& a, hipStream_t st) {
+  a.tiles = (uint32_t)((a.H + Cols<ODT>::kTile - 1) / Cols<ODT>::kTile);
+  a.cuts = a.T > kRun ? (uint32_t)((a.T + kRun - 1) / kRun) : 0u;
+  // a launch has fewer than 2^32 threads in one direction
+  a.heads = (uint32_t)((a.T + kHeads - 1) / kHeads);
+  a.wtiles = (a.tiles + kWide - 1) / kWide;
+  const uint32_t zeros = a.accumulate ? 0u : ((uint32_t)a.V * a.tiles + kPieces - 1) / kPieces;
+  const uint32_t blocks = a.cuts * a.tiles + a.heads * a.wtiles + zeros, most = 1u << 22;
+  if (blocks == 0) return;
+  const dim3 grid(blocks < most ? blocks : most, (blocks + most - 1) / most);
   hipLaunchKernelGGL((ss_grad_rows_kernel<DT, ODT>), grid, dim3(256), 0, st, a);
+  if (a.cuts) hipLaunchKernelGGL(ss_grad_join_kernel<ODT>, dim3(a.cuts, (unsigned)((a.H + 64 * Cols<ODT>::N - 1) / (64 * Cols<ODT>::N))), dim3(256), 0, st, a);
 }
 
 template <int KIND>
@@ -486,8 +555,7 @@ ss_status ss_embed_grad(const void* dout, int dtype, int T, int64_t ld, const in
   a.tokens = tokens;
   a.out = dtable;
   a.start = reinterpret_cast<int32_t*>(w + l.start);
-  a.perm = reinterpret_cast<int32_t*>(w + l.perm);
-  a.ids = reinterpret_cast<int32_t*>(w + l.ids);
+  a.list = reinterpret_cast<int4*>(w + l.list);
   a.part = reinterpret_cast<float*>(w + l.part);
   a.ld = ld;
   a.ld_out = ld_out;
@@ -499,12 +567,11 @@ ss_status ss_embed_grad(const void* dout, int dtype, int T, int64_t ld, const in
   a.wide_out = wide_rows(dtable, ld_out, out_dtype);
   a.accumulate = accumulate;
   const hipStream_t st = (hipStream_t)stream;
-  const unsigned tiles = (unsigned)((H + kCols - 1) / kCols);
   hipLaunchKernelGGL(ss_grad_sort_kernel, dim3((unsigned)((V + kRange - 1) / kRange)), dim3(kSortThreads), 0, st, a);
   if (dtype == SS_F32)
-    out_dtype == SS_F32 ? launch_sums<SS_F32, SS_F32>(a, tiles, st) : launch_sums<SS_F32, SS_BF16>(a, tiles, st);
+    out_dtype == SS_F32 ? launch_sums<SS_F32, SS_F32>(a, st) : launch_sums<SS_F32, SS_BF16>(a, st);
   else
-    out_dtype == SS_F32 ? launch_sums<SS_BF16, SS_F32>(a, tiles, st) : launch_sums<SS_BF16, SS_BF16>(a, tiles, st);
+    out_dtype == SS_F32 ? launch_sums<SS_BF16, SS_F32>(a, st) : launch_sums<SS_BF16, SS_BF16>(a, st);
   return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_HIP;
 }
 

@@ -419,7 +419,7 @@ GRAD = [
     # T, V, H, how the tokens fall
     (0, 5, 16, "even"), (1, 1, 1, "even"), (1, 300, 8, "even"), (7, 513, 60, "even"), (128, 4, 64, "even"),
     (129, 2, 72, "one"), (500, 257, 100, "few"), (1000, 700, 40, "zipf"), (1000, 3, 2056, "few"), (640, 256, 33, "blocks"),
-    (3000, 40, 24, "zipf"), (2500, 1, 16, "one"), (300, 600, 16, "none"), (900, 300, 2052, "runs"), (1025, 1025, 8, "even"), (5000, 9000, 16, "sorted"),
+    (3000, 40, 24, "zipf"), (2500, 1, 16, "one"), (300, 600, 16, "none"), (900, 300, 2052, "runs"), (809, 220, 4100, "short"), (1025, 1025, 8, "even"), (5000, 9000, 16, "sorted"),
 ]
 
 
@@ -432,6 +432,8 @@ def grad_tokens(rng, T, V, how):
         tok = rng.integers(0, min(V, 3), T)
     elif how == "zipf":
         tok = np.minimum((np.exp(rng.random(T) * np.log(V + 1)) - 1).astype(np.int64), V - 1)
+    elif how == "short":  # runs of 32 and its neighbours
+        tok = np.repeat(np.arange(20) * 11, [32, 33, 31, 1, 32, 32, 33, 33, 2, 62, 96, 97, 5, 31, 33, 64, 65, 32, 32, 63])[:T]
     elif how == "runs":  # of 64 and its neighbours, and twice that
         tok = np.repeat(np.arange(12) * 25, [64, 1, 63, 65, 64, 128, 2, 129, 127, 64, 65, 128])[:T]
     elif how == "blocks":  # runs of exactly 128 and its neighbours
@@ -441,7 +443,7 @@ def grad_tokens(rng, T, V, how):
     if how == "sorted":
         tok = np.sort(tok)
     tok = tok.astype(np.int32)
-    if how not in ("blocks", "runs"):
+    if how not in ("blocks", "runs", "short"):
         tok[rng.random(T) < 0.1] = -1
     return tok
 
