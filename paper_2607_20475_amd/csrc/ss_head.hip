@@ -13,6 +13,7 @@
 // its waves has its own vocabulary rows, whose codes go from memory to registers.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "ss_w4.hpp"
@@ -29,7 +30,9 @@ struct HeadArgs {
   int T, V, H, nb;
   int out_f32;
   int wide;               // out rows can be written NV columns at a time
-  int rows;               // tokens of a token block
+  int rows;               // hidden rows (few), tokens of a token block (more)
+  int parts;              // few: 3 where a token has four rows, its parts and one not used; else 1
+  int pitch, slab_cols;   // few: 16-byte pieces of a row in LDS; columns of a slab
   int tblocks, vblocks;   // token and vocabulary blocks
 };
 
@@ -99,6 +102,19 @@ __device__ __forceinline__ float step_scale(const Scales<KIND, CB>& s, int i, in
   }
 }
 
+// Waits for this wave's LDS accesses, then for the other waves; loads from
+// memory stay in flight over it.
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The scale of step j (32 columns) of a block whose scales are s0 and s1.
+template <int KIND>
+__device__ __forceinline__ float scale_of(uint32_t s0, uint32_t s1, int j) {
+  if constexpr (KIND == kMx) return mx_bits(j == 3 ? s0 >> 24 : s0 >> (8 * j) & 255u);
+  const int k = j / (4 / w4_groups(KIND));
+  const uint32_t x = k < 2 ? s0 : s1;
+  return __uint_as_float(k & 1 ? x & 0xFFFF0000u : x << 16);
+}
+
 __device__ __forceinline__ uint32_t dword(u32x4 v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
 
 // Writes NV consecutive columns of one token.
@@ -131,7 +147,242 @@ __device__ __forceinline__ void store_cols(const HeadArgs& a, int t, int v, cons
 }
 
 // --------------------------------------------------------------------------
-// The product
+// Up to 16 hidden rows
+// --------------------------------------------------------------------------
+// Bound by the table's read.  A workgroup of 16 waves to a CU keeps the hidden rows in LDS (all columns, or 128 KB of them
+// at a time) and has an equal share of the table's tiles of 16 rows; its waves run along the rows without
+// waiting for each other, eight 16-byte loads a lane in flight, the next block's asked for as soon as its register is
+// free, over the ends of rows.  Where all columns fit (MULTI false), the waves share the workgroup's blocks evenly, by units of
+// eight: a tile that ends up with several waves is summed through LDS, in the order of its columns.
+constexpr int kFewWaves = 16, kUnit = 8;
+constexpr int kSlabBytes = 128 * 1024;
+constexpr int kFewTiles = 2;  // MULTI: tiles of a wave whose sums stay in registers from slab to slab
+
+// 64 bytes a row of a tile's scales, 16 in each of a row's four lanes.
+__device__ __forceinline__ u32x4 load_super(const HeadArgs& a, int tile, int n, int g, int b, int sbytes, int64_t total) {
+  const int scale_row = a.nb * sbytes;
+  const int v = tile * 16 + n < a.V ? tile * 16 + n : a.V - 1;
+  const int64_t at = (int64_t)v * scale_row + b * sbytes + g * 16;
+  u32x4 s;
+  if ((int64_t)(tile * 16 + 15) * scale_row + b * sbytes + 64 <= total) {
+    __builtin_memcpy(&s, __builtin_assume_aligned(a.scales + at, 2), 16);
+  } else {  // at the end of the array: what lies in it
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t lo = 0u, hi = 0u;
+      if (at + 4 * i + 2 <= total) lo = *reinterpret_cast<const uint16_t*>(a.scales + at + 4 * i);
+      if (at + 4 * i + 4 <= total) hi = *reinterpret_cast<const uint16_t*>(a.scales + at + 4 * i + 2);
+      s[i] = lo | hi << 16;
+    }
+  }
+  return s;
+}
+
+template <int KIND, int DT, bool MULTI>
+__global__ __launch_bounds__(kFewWaves * 64) void ss_head_few_kernel(HeadArgs a) {
+  constexpr int SB = w4_scale_bytes(KIND), PER_SUPER = 64 / SB / kUnit;  // units that 64 bytes of scales cover
+  __shared__ u32x4 slab[kSlabBytes / 16];
+  __shared__ float part[MULTI ? 1 : kFewWaves][2][4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int tiles = (a.V + 15) / 16;
+  const int first = (int)((int64_t)tiles * blockIdx.x / gridDim.x), last = (int)((int64_t)tiles * (blockIdx.x + 1) / gridDim.x);
+  const int code_row = a.nb * kBlockBytes;
+  const int64_t scale_total = (int64_t)a.V * a.nb * SB;
+  const int r = n < a.rows ? n : a.rows - 1;  // rows beyond the last repeat it; their results are not written
+
+  // Hidden columns [k0, k0 + cols) to LDS: piece q of row r at q ^ (r & 15), so that 16 rows lie in different banks.
+  auto fill = [&](int k0, int cols) {
+    const int pieces = cols / 8;
+    for (int i = threadIdx.x; i < a.T * pieces; i += kFewWaves * 64) {
+      const int t = i / pieces, q = i - t * pieces;
+      const int64_t at = (int64_t)t * a.ld_h + k0 + q * 8;
+      if constexpr (DT == SS_F32) {
+        uint32_t f[8];
+        __builtin_memcpy(f, __builtin_assume_aligned(reinterpret_cast<const float*>(a.h) + at, 4), 32);
+        u32x4 y[3];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t lo[3], hi[3];
+          split3(f[2 * k], lo);
+          split3(f[2 * k + 1], hi);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) y[p][k] = lo[p] >> 16 | (hi[p] & 0xFFFF0000u);
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) slab[(4 * t + p) * a.pitch + (q ^ ((4 * t + p) & 15))] = y[p];
+      } else {
+        u32x4 x;
+        __builtin_memcpy(&x, __builtin_assume_aligned(reinterpret_cast<const uint16_t*>(a.h) + at, 2), 16);
+        slab[t * a.pitch + (q ^ (t & 15))] = x;
+      }
+    }
+  };
+
+  // The codes of unit c of a tile, block by block; blocks beyond the row's last are that one again.
+  struct Cursor {
+    const uint8_t* row;
+    int b;
+  };
+  auto cursor = [&](int tile, int c, int pb0) {
+    const int v = tile * 16 + n < a.V ? tile * 16 + n : a.V - 1;
+    return Cursor{a.codes + (int64_t)v * code_row + g * 16, pb0 + c * kUnit};
+  };
+  auto load = [&](const Cursor& at, int s) {
+    const int b = at.b + s < a.nb ? at.b + s : a.nb - 1;
+    return *reinterpret_cast<const u32x4*>(at.row + b * kBlockBytes);
+  };
+  u32x4 w[kUnit], sc, sc_next;
+
+  // Units [c0, c1) of a tile, from block pb0 of the row on (the slab's first); then comes unit c2 of tile t2, nothing if t2 < 0.
+  auto run = [&](int tile, int c0, int c1, int t2, int c2, int pb0, f32x4& tot) {
+    for (int c = c0; c < c1; ++c) {
+      const bool more = c + 1 < c1;
+      const Cursor next = cursor(more || t2 < 0 ? tile : t2, more ? c + 1 : c2, pb0);
+      if ((c - c0) % PER_SUPER == 0) {
+        sc = sc_next;
+        const bool here = c + PER_SUPER < c1;
+        if (here || t2 >= 0)
+          sc_next = load_super(a, here ? tile : t2, n, g, pb0 + (here ? c + PER_SUPER : c2) * kUnit, SB, scale_total);
+      }
+      const int piece0 = (c - c0) % PER_SUPER * (kUnit * SB / 16);
+      auto unit = [&](auto whole, auto load_next) {
+        const int left = (a.H - (pb0 + c * kUnit) * kBlockCols) / 32;  // steps to the row's end
+        uint32_t pair = 0u;
+#pragma unroll
+        for (int s = 0; s < kUnit; ++s) {
+          if (whole || 4 * s < left) {
+            // this block's scales, from the lane that has them
+            const int from = ((piece0 + s * SB / 16) * 16 + n) * 4;
+            uint32_t s0, s1 = 0u;
+            if constexpr (KIND == kInt128) {
+              if (s % 2 == 0) pair = __builtin_amdgcn_ds_bpermute(from, sc[s / 2]);
+              s0 = s % 2 ? pair >> 16 : pair;
+            } else if constexpr (KIND == kInt32) {
+              s0 = __builtin_amdgcn_ds_bpermute(from, sc[s % 2 * 2]);
+              s1 = __builtin_amdgcn_ds_bpermute(from, sc[s % 2 * 2 + 1]);
+            } else {
+              s0 = __builtin_amdgcn_ds_bpermute(from, sc[s % 4]);
+            }
+            constexpr int per_group = KIND == kMx ? 1 : 4 / w4_groups(KIND);
+            f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if (whole || 4 * s + j < left) {
+                const bf16x8 A = as_bf16x8(slab[r * a.pitch + (((c * kUnit + s) * 16 + 4 * j + g) ^ (r & 15))]);
+                const float f = scale_of<KIND>(s0, s1, j);
+                const bf16x8 W = as_bf16x8(w4_expand<KIND>(dword(w[s], j), f));
+                if constexpr (KIND == kMx) {
+                  tot = mfma(A, W, tot);
+                } else {
+                  sum = mfma(A, W, sum);
+                  if ((j + 1) % per_group == 0) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) tot[k] = __builtin_fmaf(sum[k], f, tot[k]);
+                    sum = f32x4{0.f, 0.f, 0.f, 0.f};
+                  }
+                }
+              }
+            }
+          }
+          if constexpr (decltype(load_next)::value) w[s] = load(next, s);
+        }
+      };
+      const std::true_type yes{};
+      const std::false_type no{};
+      const bool whole = (pb0 + (c + 1) * kUnit) * kBlockCols <= a.H;
+      if (more || t2 >= 0)
+        whole ? unit(yes, yes) : unit(no, yes);
+      else
+        whole ? unit(yes, no) : unit(no, no);
+    }
+  };
+  auto prime = [&](int tile, int c, int pb0) {
+    const Cursor at = cursor(tile, c, pb0);
+#pragma unroll
+    for (int s = 0; s < kUnit; ++s) w[s] = load(at, s);
+    sc_next = load_super(a, tile, n, g, pb0 + c * kUnit, SB, scale_total);
+  };
+  // Lane (n, g) of a tile has four rows of hidden states at vocabulary row n.
+  auto store = [&](int tile, const f32x4& tot) {
+    const int v = tile * 16 + n;
+    if (a.parts == 3) {  // rows 4 t .. 4 t + 2 are token t's parts
+      const float x[1] = {tot[0] + (tot[1] + tot[2])};
+      if (g < a.T) store_cols<1>(a, g, v, x);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float x[1] = {tot[k]};
+        if (g * 4 + k < a.T) store_cols<1>(a, g * 4 + k, v, x);
+      }
+    }
+  };
+
+  if constexpr (!MULTI) {
+    const int units = (a.nb + kUnit - 1) / kUnit;  // of a tile
+    const int all = (last - first) * units;
+    const int u0 = all * wave / kFewWaves, u1 = all * (wave + 1) / kFewWaves;
+    if (u0 < u1) prime(first + u0 / units, u0 % units, 0);
+    fill(0, a.H);
+    meet();
+    for (int u = u0; u < u1;) {
+      const int tile = u / units, c0 = u - tile * units, end = (tile + 1) * units < u1 ? (tile + 1) * units : u1;
+      f32x4 tot = f32x4{0.f, 0.f, 0.f, 0.f};
+      run(first + tile, c0, c0 + end - u, end < u1 ? first + tile + 1 : -1, 0, 0, tot);
+      if (end - u == units) {
+        store(first + tile, tot);
+      } else {  // slot 0: a tile that an earlier wave began; slot 1: one that this wave began
+#pragma unroll
+        for (int k = 0; k < 4; ++k) part[wave][c0 == 0][k][lane] = tot[k];
+      }
+      u = end;
+    }
+    meet();
+    // the wave that began a tile and did not end it adds what the next waves have of it
+    const int tile = (u1 - 1) / units;
+    if (u0 < u1 && u1 % units && tile * units >= u0) {
+      f32x4 tot;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) tot[k] = part[wave][1][k][lane];
+      for (int o = wave + 1; o < kFewWaves; ++o) {
+        const int o0 = all * o / kFewWaves, o1 = all * (o + 1) / kFewWaves;
+        if (o0 >= (tile + 1) * units) break;
+        if (o0 == o1) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) tot[k] += part[o][0][k][lane];
+      }
+      store(first + tile, tot);
+    }
+  } else {
+    for (int t0 = first; t0 < last; t0 += kFewWaves * kFewTiles) {
+      f32x4 tot[kFewTiles];
+#pragma unroll
+      for (int i = 0; i < kFewTiles; ++i) tot[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const int mine = t0 + wave;
+      for (int k0 = 0; k0 < a.H; k0 += a.slab_cols) {
+        const int cols = a.H - k0 < a.slab_cols ? a.H - k0 : a.slab_cols, units = (cols + kUnit * kBlockCols - 1) / (kUnit * kBlockCols);
+        const int pb0 = k0 / kBlockCols;
+        if (mine < last) prime(mine, 0, pb0);
+        meet();  // all have left the slab before
+        fill(k0, cols);
+        meet();
+#pragma unroll
+        for (int i = 0; i < kFewTiles; ++i) {
+          const int tile = mine + i * kFewWaves;
+          if (tile < last) {
+            const bool more = i + 1 < kFewTiles && tile + kFewWaves < last;
+            run(tile, 0, units, more ? tile + kFewWaves : -1, 0, pb0, tot[i]);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kFewTiles; ++i)
+        if (mine + i * kFewWaves < last) store(mine + i * kFewWaves, tot[i]);
+    }
+  }
+}
+
+// --------------------------------------------------------------------------
+// More hidden rows
 // --------------------------------------------------------------------------
 // SRC: where the hidden states come from, bfloat16 (P parts) or float32 split on the way (P = 3).
 enum HeadSource { kFromBf16 = 0, kFromF32 = 1 };
@@ -283,10 +534,6 @@ __global__ __launch_bounds__(WAVES * 64) void ss_head_kernel(HeadArgs a) {
       }
     }
   };
-  // Waits for this wave's LDS accesses, then for the other waves; loads from
-  // memory stay in flight over it.
-  auto meet = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-
   const std::true_type yes{};
   const std::false_type no{};
   load_h(0);
@@ -366,18 +613,55 @@ static ss_status launch_chunks(HeadArgs& a, hipStream_t st) {
   return launch_one<KIND, SRC, P, MT, NV, CB, WAVES>(a, st);
 }
 
+// Compute units of the current device.
+static int compute_units() {
+  static std::atomic<int> known[64];
+  int dev = 0, n = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return 0;
+  if (dev >= 0 && dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 0;
+  if (dev >= 0 && dev < 64) known[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+// Whether a table is large enough for ss_head_few_kernel: two units at least for each of its waves.  What it starts with
+// (hidden rows to LDS) and ends with (the last units of all waves at once, sums of split tiles) takes 7 us against
+// 2 of the other kernel, whose rate is lower: 33 MB (V = 32768, H = 2048, T = 1) 14.5 us against 9.7, 67 MB 17 against 18.
+static bool few_pays(const HeadArgs& a, int cus) {
+  return (int64_t)((a.V + 15) / 16) * ((a.nb + kUnit - 1) / kUnit) >= (int64_t)2 * kFewWaves * cus;
+}
+
+template <int KIND, int DT>
+static ss_status launch_few(HeadArgs& a, int cus, hipStream_t st) {
+  a.parts = DT == SS_F32 ? 3 : 1;
+  a.rows = DT == SS_F32 ? 4 * a.T : a.T;
+  // whole units: the slab's rows end with one
+  const int unit = kUnit * kBlockCols, cols = (a.nb + kUnit - 1) / kUnit * unit, fit = kSlabBytes / 2 / a.rows;
+  a.slab_cols = cols <= fit ? cols : fit / unit * unit;
+  a.pitch = a.slab_cols / 8;
+  const int tiles = (a.V + 15) / 16;
+  const dim3 grid((unsigned)(tiles < cus ? tiles : cus)), block(kFewWaves * 64);
+  if (cols <= fit)
+    hipLaunchKernelGGL((ss_head_few_kernel<KIND, DT, false>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((ss_head_few_kernel<KIND, DT, true>), grid, block, 0, st, a);
+  return SS_OK;
+}
+
+// direct: the hidden rows as the caller has them, else their parts or their copy.
 template <int KIND>
-static ss_status launch_head_f32(HeadArgs& a, bool direct, hipStream_t st) {
+static ss_status launch_head_f32(HeadArgs& a, bool direct, int cus, hipStream_t st) {
+  if (a.T <= 4 && few_pays(a, cus)) return launch_few<KIND, SS_F32>(a, cus, st);
   if (direct) return launch_chunks<KIND, kFromF32, 3, 1, 1, 2, 8>(a, st);
   if (a.T <= 16) return launch_chunks<KIND, kFromBf16, 3, 1, 1, 2, 8>(a, st);
   return launch_one<KIND, kFromBf16, 3, 2, 2, 1, 8>(a, st);
 }
 
 template <int KIND>
-static ss_status launch_head_bf16(HeadArgs& a, hipStream_t st) {
-  const int tiles = (a.T + 15) / 16;
-  if (tiles == 1) return launch_chunks<KIND, kFromBf16, 1, 1, 1, 4, 8>(a, st);
-  const int blocks = (tiles + 3) / 4, mt = (tiles + blocks - 1) / blocks;
+static ss_status launch_head_bf16(HeadArgs& a, int cus, hipStream_t st) {
+  if (a.T <= 16 && few_pays(a, cus)) return launch_few<KIND, SS_BF16>(a, cus, st);
+  const int tiles = (a.T + 15) / 16, blocks = (tiles + 3) / 4, mt = (tiles + blocks - 1) / blocks;
+  if (mt == 1) return launch_chunks<KIND, kFromBf16, 1, 1, 1, 4, 8>(a, st);
   if (mt == 2) return launch_chunks<KIND, kFromBf16, 1, 2, 2, 2, 8>(a, st);
   if (mt == 3) return launch_chunks<KIND, kFromBf16, 1, 3, 1, 2, 8>(a, st);
   return launch_chunks<KIND, kFromBf16, 1, 4, 2, 2, 8>(a, st);
@@ -417,7 +701,10 @@ ss_status ss_head_w4(const void* h, int dtype, int T, int64_t ld_h, const ss_w4*
   a.nb = w4_blocks(t->H);
   a.out_f32 = out_dtype == SS_F32;
   // few float32 rows are split by the product's own loads, more of them once, before it
-  const bool direct = wide_rows(h, ld_h, dtype) && (dtype == SS_BF16 || T <= 16);
+  const int cus = compute_units();
+  if (cus <= 0) return SS_ERR_HIP;
+  const bool few = T <= (dtype == SS_F32 ? 4 : 16) && few_pays(a, cus);  // reads rows at any address
+  const bool direct = few || (wide_rows(h, ld_h, dtype) && (dtype == SS_BF16 || T <= 16));
   if (direct) {
     a.h = h;
     a.ld_h = ld_h;
@@ -436,17 +723,17 @@ ss_status ss_head_w4(const void* h, int dtype, int T, int64_t ld_h, const ss_w4*
   ss_status done;
   if (dtype == SS_F32) {
     switch (kind) {
-      case kInt128: done = launch_head_f32<kInt128>(a, direct, st); break;
-      case kInt64: done = launch_head_f32<kInt64>(a, direct, st); break;
-      case kInt32: done = launch_head_f32<kInt32>(a, direct, st); break;
-      default: done = launch_head_f32<kMx>(a, direct, st); break;
+      case kInt128: done = launch_head_f32<kInt128>(a, direct, cus, st); break;
+      case kInt64: done = launch_head_f32<kInt64>(a, direct, cus, st); break;
+      case kInt32: done = launch_head_f32<kInt32>(a, direct, cus, st); break;
+      default: done = launch_head_f32<kMx>(a, direct, cus, st); break;
     }
   } else {
     switch (kind) {
-      case kInt128: done = launch_head_bf16<kInt128>(a, st); break;
-      case kInt64: done = launch_head_bf16<kInt64>(a, st); break;
-      case kInt32: done = launch_head_bf16<kInt32>(a, st); break;
-      default: done = launch_head_bf16<kMx>(a, st); break;
+      case kInt128: done = launch_head_bf16<kInt128>(a, cus, st); break;
+      case kInt64: done = launch_head_bf16<kInt64>(a, cus, st); break;
+      case kInt32: done = launch_head_bf16<kInt32>(a, cus, st); break;
+      default: done = launch_head_bf16<kMx>(a, cus, st); break;
     }
   }
   if (done != SS_OK) return done;
