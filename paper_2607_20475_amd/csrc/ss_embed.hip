@@ -99,6 +99,7 @@ struct GradArgs {
   float scale;
   int T, V, H;
   int wide_in, wide_out, accumulate;
+  uint32_t blocks;                     // workgroups that have something to do
   uint32_t tiles, wtiles, cuts, heads;  // column tiles, one and kWide; cuts of the list; groups of kHeads entries
 };
 
@@ -340,6 +341,7 @@ template <int DT, int ODT>
 __global__ __launch_bounds__(256) void ss_grad_rows_kernel(GradArgs a) {
   constexpr int N = Cols<ODT>::N, TILE = Cols<ODT>::kTile;
   uint32_t b = blockIdx.x + blockIdx.y * gridDim.x;
+  if (b >= a.blocks) return;
   if (b < a.cuts * a.tiles) {
     const int cut = (int)(b / a.tiles), col = (int)(b % a.tiles) * TILE + (int)threadIdx.x * N;
     const int n = a.start[a.V];
@@ -451,13 +453,13 @@ template <int DT, int ODT>
 static void launch_sums(GradArgs& a, hipStream_t st) {
   a.tiles = (uint32_t)((a.H + Cols<ODT>::kTile - 1) / Cols<ODT>::kTile);
   a.cuts = a.T > kRun ? (uint32_t)((a.T + kRun - 1) / kRun) : 0u;
-  // a launch has fewer than 2^32 threads in one direction
   a.heads = (uint32_t)((a.T + kHeads - 1) / kHeads);
   a.wtiles = (a.tiles + kWide - 1) / kWide;
-  const uint32_t zeros = a.accumulate ? 0u : ((uint32_t)a.V * a.tiles + kPieces - 1) / kPieces;
-  const uint32_t blocks = a.cuts * a.tiles + a.heads * a.wtiles + zeros, most = 1u << 22;
-  if (blocks == 0) return;
-  const dim3 grid(blocks < most ? blocks : most, (blocks + most - 1) / most);
+  const uint32_t zeros = a.accumulate ? 0u : ((uint32_t)a.V * a.tiles + kPieces - 1) / kPieces, most = 1u << 16;
+  a.blocks = a.cuts * a.tiles + a.heads * a.wtiles + zeros;
+  if (a.blocks == 0) return;
+  // in rows of 2^16: a launch has fewer than 2^32 threads in one direction
+  const dim3 grid(a.blocks < most ? a.blocks : most, (a.blocks + most - 1) / most);
   hipLaunchKernelGGL((ss_grad_rows_kernel<DT, ODT>), grid, dim3(256), 0, st, a);
   if (a.cuts) hipLaunchKernelGGL(ss_grad_join_kernel<ODT>, dim3(a.cuts, (unsigned)((a.H + 64 * Cols<ODT>::N - 1) / (64 * Cols<ODT>::N))), dim3(256), 0, st, a);
 }

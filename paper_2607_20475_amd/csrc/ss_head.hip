@@ -384,6 +384,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void ss_head_few_kernel(HeadArgs a)
 // --------------------------------------------------------------------------
 // More hidden rows
 // --------------------------------------------------------------------------
+constexpr int kAcross = 64;  // token blocks of a vocabulary block in one row of the grid
+
 // SRC: where the hidden states come from, bfloat16 (P parts) or float32 split on the way (P = 3).
 enum HeadSource { kFromBf16 = 0, kFromF32 = 1 };
 
@@ -400,9 +402,9 @@ __global__ __launch_bounds__(WAVES * 64) void ss_head_kernel(HeadArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   // Workgroups go to the eight XCDs in turn; the token blocks of a vocabulary block
   // follow one another on the same XCD, whose L2 then holds its codes.
-  const int slot = blockIdx.x >> 3;
-  const int vb = (slot / a.tblocks) * 8 + (blockIdx.x & 7), tb = slot % a.tblocks;
-  if (vb >= a.vblocks) return;
+  const int slot = blockIdx.x >> 3, across = a.tblocks < kAcross ? a.tblocks : kAcross;
+  const int vb = (slot / across) * 8 + (blockIdx.x & 7), tb = blockIdx.y * kAcross + slot % across;
+  if (vb >= a.vblocks || tb >= a.tblocks) return;
   const int v0 = (vb * WAVES + wave) * (16 * NV), t0 = tb * MT * 16;
   const int rows = a.rows;                        // of hs: the tokens of a block, at most MT * 16
   const uint8_t* code[NV];
@@ -592,23 +594,22 @@ __global__ __launch_bounds__(WAVES * 64) void ss_head_kernel(HeadArgs a) {
 // Host
 // --------------------------------------------------------------------------
 template <int KIND, int SRC, int P, int MT, int NV, int CB, int WAVES>
-static ss_status launch_one(HeadArgs& a, hipStream_t st) {
+static void launch_one(HeadArgs& a, hipStream_t st) {
   a.tblocks = (a.T + MT * 16 - 1) / (MT * 16);
   a.vblocks = (a.V + 16 * NV * WAVES - 1) / (16 * NV * WAVES);
   a.rows = MT == 1 && a.T < 16 ? a.T : MT * 16;
   const int size = a.out_f32 ? 4 : 2;
   a.wide = (uintptr_t)a.out % (NV * size) == 0 && a.ld % NV == 0;
-  const int64_t blocks = (int64_t)((a.vblocks + 7) / 8 * 8) * a.tblocks;
-  if (blocks >= (1 << 26) / WAVES) return SS_ERR_UNSUPPORTED;  // 2^32 threads
+  const int across = a.tblocks < kAcross ? a.tblocks : kAcross;
+  const dim3 grid((unsigned)((a.vblocks + 7) / 8 * 8 * across), (unsigned)((a.tblocks + kAcross - 1) / kAcross));
   const size_t lds = (size_t)2 * P * a.rows * CB * 256;
   auto kernel = ss_head_kernel<KIND, SRC, P, MT, NV, CB, WAVES>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(WAVES * 64), lds, st, a);
-  return SS_OK;
+  hipLaunchKernelGGL(kernel, grid, dim3(WAVES * 64), lds, st, a);
 }
 
 // CB blocks at a time where the row has as many
 template <int KIND, int SRC, int P, int MT, int NV, int CB, int WAVES>
-static ss_status launch_chunks(HeadArgs& a, hipStream_t st) {
+static void launch_chunks(HeadArgs& a, hipStream_t st) {
   if (a.nb < CB) return launch_one<KIND, SRC, P, MT, NV, 1, WAVES>(a, st);
   return launch_one<KIND, SRC, P, MT, NV, CB, WAVES>(a, st);
 }
@@ -632,7 +633,7 @@ static bool few_pays(const HeadArgs& a, int cus) {
 }
 
 template <int KIND, int DT>
-static ss_status launch_few(HeadArgs& a, int cus, hipStream_t st) {
+static void launch_few(HeadArgs& a, int cus, hipStream_t st) {
   a.parts = DT == SS_F32 ? 3 : 1;
   a.rows = DT == SS_F32 ? 4 * a.T : a.T;
   // whole units: the slab's rows end with one
@@ -645,12 +646,11 @@ static ss_status launch_few(HeadArgs& a, int cus, hipStream_t st) {
     hipLaunchKernelGGL((ss_head_few_kernel<KIND, DT, false>), grid, block, 0, st, a);
   else
     hipLaunchKernelGGL((ss_head_few_kernel<KIND, DT, true>), grid, block, 0, st, a);
-  return SS_OK;
 }
 
 // direct: the hidden rows as the caller has them, else their parts or their copy.
 template <int KIND>
-static ss_status launch_head_f32(HeadArgs& a, bool direct, int cus, hipStream_t st) {
+static void launch_head_f32(HeadArgs& a, bool direct, int cus, hipStream_t st) {
   if (a.T <= 4 && few_pays(a, cus)) return launch_few<KIND, SS_F32>(a, cus, st);
   if (direct) return launch_chunks<KIND, kFromF32, 3, 1, 1, 2, 8>(a, st);
   if (a.T <= 16) return launch_chunks<KIND, kFromBf16, 3, 1, 1, 2, 8>(a, st);
@@ -658,7 +658,7 @@ static ss_status launch_head_f32(HeadArgs& a, bool direct, int cus, hipStream_t 
 }
 
 template <int KIND>
-static ss_status launch_head_bf16(HeadArgs& a, int cus, hipStream_t st) {
+static void launch_head_bf16(HeadArgs& a, int cus, hipStream_t st) {
   if (a.T <= 16 && few_pays(a, cus)) return launch_few<KIND, SS_BF16>(a, cus, st);
   const int tiles = (a.T + 15) / 16, blocks = (tiles + 3) / 4, mt = (tiles + blocks - 1) / blocks;
   if (mt == 1) return launch_chunks<KIND, kFromBf16, 1, 1, 1, 4, 8>(a, st);
@@ -720,23 +720,21 @@ ss_status ss_head_w4(const void* h, int dtype, int T, int64_t ld_h, const ss_w4*
     a.ld_h = t->H;
     a.part = n;
   }
-  ss_status done;
   if (dtype == SS_F32) {
     switch (kind) {
-      case kInt128: done = launch_head_f32<kInt128>(a, direct, cus, st); break;
-      case kInt64: done = launch_head_f32<kInt64>(a, direct, cus, st); break;
-      case kInt32: done = launch_head_f32<kInt32>(a, direct, cus, st); break;
-      default: done = launch_head_f32<kMx>(a, direct, cus, st); break;
+      case kInt128: launch_head_f32<kInt128>(a, direct, cus, st); break;
+      case kInt64: launch_head_f32<kInt64>(a, direct, cus, st); break;
+      case kInt32: launch_head_f32<kInt32>(a, direct, cus, st); break;
+      default: launch_head_f32<kMx>(a, direct, cus, st); break;
     }
   } else {
     switch (kind) {
-      case kInt128: done = launch_head_bf16<kInt128>(a, cus, st); break;
-      case kInt64: done = launch_head_bf16<kInt64>(a, cus, st); break;
-      case kInt32: done = launch_head_bf16<kInt32>(a, cus, st); break;
-      default: done = launch_head_bf16<kMx>(a, cus, st); break;
+      case kInt128: launch_head_bf16<kInt128>(a, cus, st); break;
+      case kInt64: launch_head_bf16<kInt64>(a, cus, st); break;
+      case kInt32: launch_head_bf16<kInt32>(a, cus, st); break;
+      default: launch_head_bf16<kMx>(a, cus, st); break;
     }
   }
-  if (done != SS_OK) return done;
   return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_HIP;
 }
 

@@ -336,8 +336,14 @@ def test_head_of_large_tables(ssb, fmt, group, dtype, T):
         table = ssb.W4(codes, scales, V, H, fmt, group)
         say(f"[head large] {fmt}{group} {dtype} T={T} V={V} H={H}")
         h = torch.empty(T, H + 3, device="cuda").normal_(generator=g).to(dtype)[:, 1:H + 1]  # rows at odd addresses
+        if T >= 4:
+            h[1, H // 2], h[2, H - 1] = float("inf"), float("nan")  # stay in their rows
         out = torch.full((T, V + 1), 77.0, device="cuda")
         ssb.head_w4(h, table, out=out[:, :V])
+        if T >= 4:
+            assert not torch.isfinite(out[1:3, :V]).any()
+            h[1:3] = 0
+            out[1:3, :V] = 0
         W = ssb.embed(torch.arange(V, dtype=torch.int32, device="cuda"), table, dtype=F32)
         h64 = h.double()
         for r in range(0, V, 32768):
@@ -455,11 +461,59 @@ def grad64(dout, tok, V, scale):
     return ref, S, n
 
 
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits(ssb):
+    """Tables, gradients and logits of more than 4 GB: their last rows, against the same rows of a small call."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(15)
+    V, H = 560000, 4096
+    say("[4 GB] lookup")
+    table = torch.zeros(V, H, dtype=BF16, device="cuda")
+    table[-40:].normal_(generator=g)
+    tok = torch.tensor([V - 1, 5, V - 40, V, V - 7], dtype=torch.int32, device="cuda")
+    out = ssb.embed(tok, table)
+    assert torch.equal(out[[0, 2, 4]], table[[V - 1, V - 40, V - 7]]) and not out[[1, 3]].any()
+    say("[4 GB] gradient")
+    d = torch.empty(5, H, device="cuda").normal_(generator=g)
+    dW = torch.full((V, H), 3.0, device="cuda")
+    ssb.embed_grad(d, tok, V, out=dW)
+    assert torch.equal(dW[[V - 1, 5, V - 40, V - 7]], d[[0, 1, 2, 4]])
+    dW[[V - 1, 5, V - 40, V - 7]] = 0
+    assert int(torch.count_nonzero(dW)) == 0
+    del table, dW
+    say("[4 GB] quantiser, head, lookup in 4 bits")
+    V, H = 1 << 20, 8704
+    w = torch.zeros(V, H, dtype=BF16, device="cuda")
+    w[-100:].normal_(generator=g)
+    t = ssb.quantize_w4(w, fmt="mx", group=32)
+    small = ssb.quantize_w4(w[-100:].contiguous(), fmt="mx", group=32)
+    assert torch.equal(t.codes[-100:], small.codes) and torch.equal(t.scales[-100:], small.scales)
+    del w
+    for T in (2, 20):
+        h = torch.empty(T, H, dtype=BF16, device="cuda").normal_(generator=g)
+        big, few = ssb.head_w4(h, t, dtype=F32), ssb.head_w4(h, small, dtype=F32)
+        # a sum of one row's products in another order
+        assert (big[:, -100:] - few).abs().max() <= (32 + H / 32 + 24) * 2.0 ** -22 * 6 * H
+        assert int(torch.count_nonzero(big[:, :-100])) == 0 and big[:, -100:].abs().min() > 0
+    tok = torch.arange(V - 100, V, dtype=torch.int32, device="cuda")
+    assert torch.equal(ssb.embed(tok, t), ssb.embed(tok - (V - 100), small))
+    del t, big, few
+    say("[4 GB] logits")
+    T, H = 2300, 32
+    w = torch.empty(V, H, dtype=BF16, device="cuda").normal_(generator=g)
+    t = ssb.quantize_w4(w, fmt="int", group=32)
+    h = torch.empty(T, H, dtype=BF16, device="cuda").normal_(generator=g)
+    big = ssb.head_w4(h, t)
+    small = ssb.W4(t.codes[-64:].clone(), t.scales[-64:].clone(), 64, H, "int", 32)
+    assert torch.equal(big[-30:, -64:], ssb.head_w4(h[-30:], small))
+
+
 GRAD = [
     # T, V, H, how the tokens fall
     (0, 5, 16, "even"), (1, 1, 1, "even"), (1, 300, 8, "even"), (7, 513, 60, "even"), (128, 4, 64, "even"),
     (129, 2, 72, "one"), (500, 257, 100, "few"), (1000, 700, 40, "zipf"), (1000, 3, 2056, "few"), (640, 256, 33, "blocks"),
     (3000, 40, 24, "zipf"), (2500, 1, 16, "one"), (300, 600, 16, "none"), (900, 300, 2052, "runs"), (809, 220, 4100, "short"), (1025, 1025, 8, "even"), (5000, 9000, 16, "sorted"),
+    (200100, 500, 8, "even"),
 ]
 
 
