@@ -663,8 +663,16 @@ static void launch_head_bf16(HeadArgs& a, int cus, hipStream_t st) {
   const int tiles = (a.T + 15) / 16, blocks = (tiles + 3) / 4, mt = (tiles + blocks - 1) / blocks;
   if (mt == 1) return launch_chunks<KIND, kFromBf16, 1, 1, 1, 4, 8>(a, st);
   if (mt == 2) return launch_chunks<KIND, kFromBf16, 1, 2, 2, 2, 8>(a, st);
-  if (mt == 3) return launch_chunks<KIND, kFromBf16, 1, 3, 1, 2, 8>(a, st);
-  return launch_chunks<KIND, kFromBf16, 1, 4, 2, 2, 8>(a, st);
+  // Integers keep a group's sums beside the row's: with more tiles a wave they leave too few registers.  V = 131072, H = 4096, by
+  // (NV, WAVES), in us:  T = 48: int32 (1, 8) 104, (2, 8) 103; mx (1, 8) 94, (2, 8) 80.  T = 64: int128 (1, 16) 86,
+  // (2, 8) 88; int32 109, 116; mx (1, 16) 91, (4, 8) 89.  T = 320: int128 (1, 16) 381, (2, 8) 466, (4, 8) 1080; mx (1, 16) 381, (4, 8) 347.
+  if constexpr (KIND == kMx) {
+    if (mt == 3) return launch_chunks<KIND, kFromBf16, 1, 3, 2, 2, 8>(a, st);
+    launch_chunks<KIND, kFromBf16, 1, 4, 4, 2, 8>(a, st);
+  } else {
+    if (mt == 3) return launch_chunks<KIND, kFromBf16, 1, 3, 1, 2, 8>(a, st);
+    launch_chunks<KIND, kFromBf16, 1, 4, 1, 2, 16>(a, st);
+  }
 }
 
 }  // namespace ss
