@@ -421,7 +421,7 @@ __global__ __launch_bounds__(WAVES * 64) void ss_head_kernel(HeadArgs a) {
   // Chunk c starts at block c * CB; the last one is moved back into the row, and skips the blocks that the
   // chunk before it had.  So every load is made, whole, in every turn of the loop: behind a condition,
   // the compiler would have to wait for all loads in flight where its branches meet.
-    auto base = [&](int c) { return c * CB < a.nb - CB ? c * CB : a.nb - CB; };
+  auto base = [&](int c) { return c * CB < a.nb - CB ? c * CB : a.nb - CB; };
 
   // Hidden states: piece q of row r lies at slot q ^ (r & 15), so that the 16 rows of an operand lie in
   // different banks.
@@ -607,13 +607,6 @@ static void launch_one(HeadArgs& a, hipStream_t st) {
   hipLaunchKernelGGL(kernel, grid, dim3(WAVES * 64), lds, st, a);
 }
 
-// CB blocks at a time where the row has as many
-template <int KIND, int SRC, int P, int MT, int NV, int CB, int WAVES>
-static void launch_chunks(HeadArgs& a, hipStream_t st) {
-  if (a.nb < CB) return launch_one<KIND, SRC, P, MT, NV, 1, WAVES>(a, st);
-  return launch_one<KIND, SRC, P, MT, NV, CB, WAVES>(a, st);
-}
-
 // Compute units of the current device.
 static int compute_units() {
   static std::atomic<int> known[64];
@@ -648,31 +641,60 @@ static void launch_few(HeadArgs& a, int cus, hipStream_t st) {
     hipLaunchKernelGGL((ss_head_few_kernel<KIND, DT, true>), grid, block, 0, st, a);
 }
 
-// direct: the hidden rows as the caller has them, else their parts or their copy.
+// direct: the hidden rows as the caller has them, else their parts or their copy.  V = 32768, H = 2048, T = 32: tiles (NV, CB, WAVES)
+// (2, 1, 8) 30 us, (1, 2, 8) 20; V = 131072, H = 4096: 112 and 144.
 template <int KIND>
 static void launch_head_f32(HeadArgs& a, bool direct, int cus, hipStream_t st) {
   if (a.T <= 4 && few_pays(a, cus)) return launch_few<KIND, SS_F32>(a, cus, st);
-  if (direct) return launch_chunks<KIND, kFromF32, 3, 1, 1, 2, 8>(a, st);
-  if (a.T <= 16) return launch_chunks<KIND, kFromBf16, 3, 1, 1, 2, 8>(a, st);
+  const bool columns = a.nb >= 2, small = (int64_t)((a.V + 15) / 16) * ((a.T + 31) / 32) <= (int64_t)8 * cus;
+  if (direct && columns) return launch_one<KIND, kFromF32, 3, 1, 1, 2, 8>(a, st);
+  if (direct) return launch_one<KIND, kFromF32, 3, 1, 1, 1, 8>(a, st);
+  if (a.T <= 16 && columns) return launch_one<KIND, kFromBf16, 3, 1, 1, 2, 8>(a, st);
+  if (a.T <= 16) return launch_one<KIND, kFromBf16, 3, 1, 1, 1, 8>(a, st);
+  if (small && columns) return launch_one<KIND, kFromBf16, 3, 2, 1, 2, 8>(a, st);
   return launch_one<KIND, kFromBf16, 3, 2, 2, 1, 8>(a, st);
 }
 
+// Tiles of 16 tokens and of 16 vocabulary rows a workgroup.  The more of them, the fewer times hidden rows and codes are read;
+// but a table that gives less than a workgroup to each compute unit is cut finer.  Integers keep a group's sums beside the
+// row's: more than one tile of vocabulary rows a wave leaves them too few registers.  Measured, us, by (NV, CB, WAVES):
+//   V = 32768, H = 2048   T = 16: (1, 4, 8) 9.6, (1, 4, 4) 10.4.   T = 32: (1, 4, 8) 11.4, (1, 2, 16) 17.  T = 64: (1, 2, 8) 15, (1, 2, 16) 19.5,
+//                         mx (4, 2, 8) 37.   V = 16384: T = 16: (1, 4, 8) 8.4, (1, 4, 4) 7.3.
+//   V = 65536, H = 4096   T = 32: (1, 4, 8) 37, (1, 2, 16) 33.  T = 64: (1, 2, 8) 55, (1, 2, 16) 40.
+//   V = 131072, H = 4096  T = 32: (1, 2, 16) 77, (2, 2, 8) 78 to 105.  T = 48, mx: (2, 2, 8) 76, (1, 2, 16) 88; int128 (1, 2, 8) 88, (1, 2, 16) 84
+//                         (V = 200003, H = 2880, int32: 118 and 126: 3.05 rounds of the chip, 16 waves leave more behind in the last).
+//                         T = 64, mx: (4, 2, 8) 89, (1, 2, 16) 91.  T = 320: mx (4, 2, 8) 347, (1, 2, 16) 381; int128 1080 and 381.
 template <int KIND>
 static void launch_head_bf16(HeadArgs& a, int cus, hipStream_t st) {
   if (a.T <= 16 && few_pays(a, cus)) return launch_few<KIND, SS_BF16>(a, cus, st);
   const int tiles = (a.T + 15) / 16, blocks = (tiles + 3) / 4, mt = (tiles + blocks - 1) / blocks;
-  if (mt == 1) return launch_chunks<KIND, kFromBf16, 1, 1, 1, 4, 8>(a, st);
-  if (mt == 2) return launch_chunks<KIND, kFromBf16, 1, 2, 2, 2, 8>(a, st);
-  // Integers keep a group's sums beside the row's: with more tiles a wave they leave too few registers.  V = 131072, H = 4096, by
-  // (NV, WAVES), in us:  T = 48: int32 (1, 8) 104, (2, 8) 103; mx (1, 8) 94, (2, 8) 80.  T = 64: int128 (1, 16) 86,
-  // (2, 8) 88; int32 109, 116; mx (1, 16) 91, (4, 8) 89.  T = 320: int128 (1, 16) 381, (2, 8) 466, (4, 8) 1080; mx (1, 16) 381, (4, 8) 347.
-  if constexpr (KIND == kMx) {
-    if (mt == 3) return launch_chunks<KIND, kFromBf16, 1, 3, 2, 2, 8>(a, st);
-    launch_chunks<KIND, kFromBf16, 1, 4, 4, 2, 8>(a, st);
-  } else {
-    if (mt == 3) return launch_chunks<KIND, kFromBf16, 1, 3, 1, 2, 8>(a, st);
-    launch_chunks<KIND, kFromBf16, 1, 4, 1, 2, 16>(a, st);
+  const int64_t work = (int64_t)((a.V + 15) / 16) * ((tiles + mt - 1) / mt);  // tiles of vocabulary rows, for each token block
+  if (a.nb < 4) {  // fewer blocks than a chunk
+    if (mt == 1) return launch_one<KIND, kFromBf16, 1, 1, 1, 1, 8>(a, st);
+    if (mt == 2) return launch_one<KIND, kFromBf16, 1, 2, 1, 1, 8>(a, st);
+    if (mt == 3) return launch_one<KIND, kFromBf16, 1, 3, 1, 1, 8>(a, st);
+    return launch_one<KIND, kFromBf16, 1, 4, 1, 1, 8>(a, st);
   }
+  if (mt == 1) {
+    if (work <= (int64_t)4 * cus) return launch_one<KIND, kFromBf16, 1, 1, 1, 4, 4>(a, st);
+    return launch_one<KIND, kFromBf16, 1, 1, 1, 4, 8>(a, st);
+  }
+  const bool small = work <= (int64_t)8 * cus;
+  if (mt == 2) {
+    if (small) return launch_one<KIND, kFromBf16, 1, 2, 1, 4, 8>(a, st);
+    return launch_one<KIND, kFromBf16, 1, 2, 1, 2, 16>(a, st);
+  }
+  if (mt == 3) {
+    if constexpr (KIND == kMx) {
+      if (!small) return launch_one<KIND, kFromBf16, 1, 3, 2, 2, 8>(a, st);
+    }
+    return launch_one<KIND, kFromBf16, 1, 3, 1, 2, 8>(a, st);
+  }
+  if (small) return launch_one<KIND, kFromBf16, 1, 4, 1, 2, 8>(a, st);
+  if constexpr (KIND == kMx) {
+    if (work >= (int64_t)32 * cus) return launch_one<KIND, kFromBf16, 1, 4, 4, 2, 8>(a, st);
+  }
+  return launch_one<KIND, kFromBf16, 1, 4, 1, 2, 16>(a, st);
 }
 
 }  // namespace ss

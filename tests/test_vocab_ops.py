@@ -355,6 +355,43 @@ def test_head_of_large_tables(ssb, fmt, group, dtype, T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", KINDS)
+@pytest.mark.parametrize("dtype,T", [(BF16, 9), (BF16, 20), (BF16, 41), (BF16, 64), (BF16, 100), (F32, 11), (F32, 27), (F32, 70)])
+def test_head_of_large_tables_with_more_rows(ssb, fmt, group, dtype, T):
+    """The same with every number of token tiles, for tables that give each compute unit less than a workgroup, more
+    than one, and many (columns end inside a block and inside a chunk)."""
+    g = torch.Generator(device="cuda")
+    for V, H in ((12301, 1824), (30011, 800), (40003, 928), (131077, 672)):
+        H = (H + group - 1) // group * group
+        g.manual_seed(V + H)
+        nb = (H + 127) // 128
+        codes = torch.randint(0, 256, (V, 64 * nb), dtype=torch.uint8, device="cuda", generator=g)
+        if fmt == "mx":
+            scales = torch.randint(115, 125, (V, nb * 4), dtype=torch.uint8, device="cuda", generator=g)
+            scales[:, H // 32:] = 255
+        else:
+            scales = torch.empty(V, nb * 128 // group, device="cuda").uniform_(0.001, 0.02, generator=g).to(BF16)
+            scales[:, H // group:] = float("nan")
+        table = ssb.W4(codes, scales, V, H, fmt, group)
+        say(f"[head large] {fmt}{group} {dtype} T={T} V={V} H={H}")
+        h = torch.empty(T, H, device="cuda").normal_(generator=g).to(dtype)
+        h[1, H // 2], h[2, H - 1] = float("inf"), float("nan")  # stay in their rows
+        out = torch.full((T, V + 3), 77.0, device="cuda")
+        ssb.head_w4(h, table, out=out[:, :V])
+        assert not torch.isfinite(out[1:3, :V]).any()
+        h[1:3] = 0
+        out[1:3, :V] = 0
+        W = ssb.embed(torch.arange(V, dtype=torch.int32, device="cuda"), table, dtype=F32)
+        h64 = h.double()
+        for r in range(0, V, 32768):
+            w = W[r:r + 32768].double()
+            ref, S = h64 @ w.T, h64.abs() @ w.abs().T
+            tol = (32 + (3 if dtype == F32 else 1) * H / 32 + 24) * 2.0 ** -23 * S + U[F32] * ref.abs()
+            assert ((out[:, r:min(r + 32768, V)].double() - ref).abs() <= tol).all(), (V, H)
+        assert (out[:, V:] == 77).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [3, 40])
 def test_head_takes_float32_whole(ssb, T):
     """Hidden states that differ beyond bfloat16: the result keeps what float32 has.  A table row of a single one
