@@ -392,6 +392,9 @@ size_t ss_head_w4_bytes(int T, int H, int dtype);
  *     logits[t, v] = sum_k h[t, k] * W[v, k]
  * with products exact and sums in float32 (float32 hidden states are taken whole, as three
  * bfloat16 parts), rounded once to `out_dtype`.  The sampler's entry points read the result.
+ * SS_W4_INT: a group's products with the integers are summed before the group's scale, so hidden states
+ * beyond 2^116 may overflow where the scaled sum would not.  Bits of hidden states below 2^-126 may be
+ * taken as zero.
  * A row does not depend on the values of the other rows.
  *   h       [T, ld_h] of `dtype` (SS_F32 or SS_BF16), 0 <= T <= SS_MAX_T, ld_h >= t->H.
  *   logits  [T, ld] of `out_dtype`, ld >= t->V; columns beyond V are left as they were.

@@ -655,15 +655,42 @@ static void launch_head_f32(HeadArgs& a, bool direct, int cus, hipStream_t st) {
   return launch_one<KIND, kFromBf16, 3, 2, 2, 1, 8>(a, st);
 }
 
-// Tiles of 16 tokens and of 16 vocabulary rows a workgroup.  The more of them, the fewer times hidden rows and codes are read;
-// but a table that gives less than a workgroup to each compute unit is cut finer.  Integers keep a group's sums beside the
-// row's: more than one tile of vocabulary rows a wave leaves them too few registers.  Measured, us, by (NV, CB, WAVES):
-//   V = 32768, H = 2048   T = 16: (1, 4, 8) 9.6, (1, 4, 4) 10.4.   T = 32: (1, 4, 8) 11.4, (1, 2, 16) 17.  T = 64: (1, 2, 8) 15, (1, 2, 16) 19.5,
-//                         mx (4, 2, 8) 37.   V = 16384: T = 16: (1, 4, 8) 8.4, (1, 4, 4) 7.3.
-//   V = 65536, H = 4096   T = 32: (1, 4, 8) 37, (1, 2, 16) 33.  T = 64: (1, 2, 8) 55, (1, 2, 16) 40.
-//   V = 131072, H = 4096  T = 32: (1, 2, 16) 77, (2, 2, 8) 78 to 105.  T = 48, mx: (2, 2, 8) 76, (1, 2, 16) 88; int128 (1, 2, 8) 88, (1, 2, 16) 84
-//                         (V = 200003, H = 2880, int32: 118 and 126: 3.05 rounds of the chip, 16 waves leave more behind in the last).
-//                         T = 64, mx: (4, 2, 8) 89, (1, 2, 16) 91.  T = 320: mx (4, 2, 8) 347, (1, 2, 16) 381; int128 1080 and 381.
+// Large tables: 16, 14 or 12 waves a workgroup, one of which a compute unit holds, by the time that the chip's rounds of
+// them take, which goes with the waves and 8 more (starting, and the hidden rows' share).  Measured, us, T = 29 / 64, int128:
+//   V = 131072, H = 4096 (32 tiles a compute unit)  16 waves 67 / 88, 14 waves 89, 12 waves 75
+//   V = 98304, H = 4096 (24)                        59 / 76, 58 / 74, 53 / 69
+//   V = 161103, H = 4736 (39.3)                     112 / 136 (mx 153), 107 / 139 (mx 133), 118 / 159 (mx 144)
+// E2M1 has no sums of groups beside the row's, which leaves registers for four tiles of vocabulary rows a wave: T = 64, V = 131072 89
+// against 91 of 16 waves, V = 161103 226 against 133 of 14; T = 320, V = 131072 347 against 381.  Integers spill there (517).
+template <int KIND, int MT>
+static void launch_rounds(HeadArgs& a, int64_t work, int cus, hipStream_t st) {
+  auto cost = [&](int tiles, int each) { return (work + (int64_t)tiles * cus - 1) / ((int64_t)tiles * cus) * each; };
+  const int64_t c16 = cost(16, 24), c14 = cost(14, 22), c12 = cost(12, 20), least = c12 < c14 ? c12 : c14;
+  if constexpr (KIND == kMx && MT == 4) {
+    if (cost(32, 48) <= (least < c16 ? least : c16)) return launch_one<KIND, kFromBf16, 1, MT, 4, 2, 8>(a, st);
+  }
+  if (c16 <= least) return launch_one<KIND, kFromBf16, 1, MT, 1, 2, 16>(a, st);
+  if (c14 <= c12) return launch_one<KIND, kFromBf16, 1, MT, 1, 2, 14>(a, st);
+  return launch_one<KIND, kFromBf16, 1, MT, 1, 2, 12>(a, st);
+}
+
+// 33 to 48 tokens: two workgroups of 8 waves a compute unit, which leave less behind in the last round (T = 37, V = 200003: int128 98,
+// mx 102; 16 waves 103, 111; V = 131072: 81, 80).  E2M1 takes two tiles of vocabulary rows a wave where that fills its
+// rounds of 16 tiles to a tenth: V = 131072 79 against 88; V = 98304, one round and a half, 70 against 68.
+template <int KIND>
+static void launch_48(HeadArgs& a, int64_t work, int cus, hipStream_t st) {
+  if constexpr (KIND == kMx) {
+    const int64_t round = (int64_t)16 * cus;
+    if (10 * ((work + round - 1) / round * round) <= 11 * work) return launch_one<KIND, kFromBf16, 1, 3, 2, 2, 8>(a, st);
+  }
+  return launch_one<KIND, kFromBf16, 1, 3, 1, 2, 8>(a, st);
+}
+
+// Tiles of 16 tokens and waves a workgroup.  The more of them, the fewer times hidden rows and codes are read; but a table that
+// gives less than a workgroup to each compute unit is cut finer.  Measured, us, by (CB, WAVES):
+//   V = 16384, H = 2048   T = 16: (4, 8) 8.4, (4, 4) 7.3.
+//   V = 32768, H = 2048   T = 16: (4, 8) 9.6, (4, 4) 10.4.  T = 32: (4, 8) 11.4, (2, 16) 17.  T = 64: (2, 8) 15, (2, 16) 19.5.
+//   V = 65536, H = 4096   T = 32: (4, 8) 37, (2, 16) 33.  T = 64: (2, 8) 55, (2, 16) 40.
 template <int KIND>
 static void launch_head_bf16(HeadArgs& a, int cus, hipStream_t st) {
   if (a.T <= 16 && few_pays(a, cus)) return launch_few<KIND, SS_BF16>(a, cus, st);
@@ -679,22 +706,13 @@ static void launch_head_bf16(HeadArgs& a, int cus, hipStream_t st) {
     if (work <= (int64_t)4 * cus) return launch_one<KIND, kFromBf16, 1, 1, 1, 4, 4>(a, st);
     return launch_one<KIND, kFromBf16, 1, 1, 1, 4, 8>(a, st);
   }
-  const bool small = work <= (int64_t)8 * cus;
-  if (mt == 2) {
-    if (small) return launch_one<KIND, kFromBf16, 1, 2, 1, 4, 8>(a, st);
-    return launch_one<KIND, kFromBf16, 1, 2, 1, 2, 16>(a, st);
+  if (mt == 3) return launch_48<KIND>(a, work, cus, st);
+  if (work <= (int64_t)8 * cus) {
+    if (mt == 2) return launch_one<KIND, kFromBf16, 1, 2, 1, 4, 8>(a, st);
+    return launch_one<KIND, kFromBf16, 1, 4, 1, 2, 8>(a, st);
   }
-  if (mt == 3) {
-    if constexpr (KIND == kMx) {
-      if (!small) return launch_one<KIND, kFromBf16, 1, 3, 2, 2, 8>(a, st);
-    }
-    return launch_one<KIND, kFromBf16, 1, 3, 1, 2, 8>(a, st);
-  }
-  if (small) return launch_one<KIND, kFromBf16, 1, 4, 1, 2, 8>(a, st);
-  if constexpr (KIND == kMx) {
-    if (work >= (int64_t)32 * cus) return launch_one<KIND, kFromBf16, 1, 4, 4, 2, 8>(a, st);
-  }
-  return launch_one<KIND, kFromBf16, 1, 4, 1, 2, 16>(a, st);
+  if (mt == 2) return launch_rounds<KIND, 2>(a, work, cus, st);
+  return launch_rounds<KIND, 4>(a, work, cus, st);
 }
 
 }  // namespace ss

@@ -361,7 +361,7 @@ def test_head_of_large_tables_with_more_rows(ssb, fmt, group, dtype, T):
     """The same with every number of token tiles, for tables that give each compute unit less than a workgroup, more
     than one, and many (columns end inside a block and inside a chunk)."""
     g = torch.Generator(device="cuda")
-    for V, H in ((12301, 1824), (30011, 800), (40003, 928), (131077, 672)):
+    for V, H in ((12301, 1824), (30011, 800), (40003, 928), (95003, 544), (131077, 672), (161103, 1184)):
         H = (H + group - 1) // group * group
         g.manual_seed(V + H)
         nb = (H + 127) // 128
