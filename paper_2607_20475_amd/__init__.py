@@ -5,3 +5,4 @@ The computation lives in ``libss.so`` (hand-written HIP for gfx950, C ABI in
 """
 from . import binding  # noqa: F401
 from .binding import topk, sample, verify, process_logits, Params, workspace  # noqa: F401
+from .binding import W4, quantize_w4, head_w4, embed, embed_grad  # noqa: F401

@@ -149,7 +149,8 @@ __device__ __forceinline__ void store_cols(const HeadArgs& a, int t, int v, cons
 // --------------------------------------------------------------------------
 // Up to 16 hidden rows
 // --------------------------------------------------------------------------
-// Bound by the table's read.  A workgroup of 16 waves to a CU keeps the hidden rows in LDS (all columns, or 128 KB of them
+// Bound by the table's read: V = 262144, H = 8192, T = 16 mx 217 us, 5.3 TB/s; V = 32768, H = 4096, four float32 rows 17.5 us, 4.1
+// TB/s.  A workgroup of 16 waves to a CU keeps the hidden rows in LDS (all columns, or 128 KB of them
 // at a time) and has an equal share of the table's tiles of 16 rows; its waves run along the rows without
 // waiting for each other, eight 16-byte loads a lane in flight, the next block's asked for as soon as its register is
 // free, over the ends of rows.  Where all columns fit (MULTI false), the waves share the workgroup's blocks evenly, by units of
@@ -389,8 +390,12 @@ constexpr int kAcross = 64;  // token blocks of a vocabulary block in one row of
 // SRC: where the hidden states come from, bfloat16 (P parts) or float32 split on the way (P = 3).
 enum HeadSource { kFromBf16 = 0, kFromF32 = 1 };
 
-// Threads have a workgroup of WAVES waves; each wave has NV tiles of 16 vocabulary rows and all MT tiles of
-// 16 tokens, and takes CB blocks of columns (a chunk) at a time.
+// A workgroup has WAVES waves; each wave has NV tiles of 16 vocabulary rows and all MT tiles of 16 tokens, and takes CB blocks
+// of columns (a chunk) at a time, codes of the next chunk in flight.  Up to 16 tokens it is bound by the table's read and the
+// start of its workgroups (V = 32768, H = 2048, T = 1: 8.7 us, 4.0 TB/s), beyond by the issue of vector instructions: a step of
+// 32 columns takes 7 to expand the codes (4 for E2M1), 4 MT / (group / 32) to scale sums (none for E2M1) and a few for
+// addresses, beside MT matrix instructions of 16 cycles.  V = 131072, H = 4096: T = 64 int128 87 us, 790 TFLOP/s; T = 320 mx 342
+// us, 1000 TFLOP/s (a library's product of bfloat16 matrices of these sizes: 353 us); V = 200003, H = 2880, T = 37 int32: 117 us.
 template <int KIND, int SRC, int P, int MT, int NV, int CB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void ss_head_kernel(HeadArgs a) {
   constexpr int THREADS = WAVES * 64;
