@@ -392,6 +392,47 @@ def test_head_of_large_tables_with_more_rows(ssb, fmt, group, dtype, T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", KINDS)
+def test_the_widest_rows(ssb, fmt, group):
+    """Rows of 65536 columns, the most there are, through every operator; tables that fill the chip and that do not."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    H = 65536
+    for V in (37, 2049):
+        w = torch.empty(V, H, device="cuda").normal_(generator=g)
+        table = ssb.quantize_w4(w, fmt=fmt, group=group, values=w)
+        W = ssb.embed(torch.arange(V, dtype=torch.int32, device="cuda"), table, dtype=F32)
+        assert torch.equal(W, w)
+        for dtype, T in ((BF16, 1), (BF16, 16), (BF16, 33), (F32, 1), (F32, 3), (F32, 17)):
+            say(f"[wide] {fmt}{group} V={V} {dtype} T={T}")
+            h = torch.empty(T, H, device="cuda").normal_(generator=g).to(dtype)
+            out = ssb.head_w4(h, table, dtype=F32)
+            ref, S = h.double() @ W.double().T, h.double().abs() @ W.double().abs().T
+            tol = (32 + (3 if dtype == F32 else 1) * H / 32 + 24) * 2.0 ** -23 * S + U[F32] * ref.abs()
+            assert ((out.double() - ref).abs() <= tol).all(), (V, dtype, T)
+    tokens = torch.tensor([4, -1, 4, 36, 0] + [7] * 70, dtype=torch.int32, device="cuda")
+    d = torch.empty(len(tokens), H, device="cuda").normal_(generator=g)
+    grad = ssb.embed_grad(d, tokens, 37)
+    for v, where in ((4, [0, 2]), (36, [3]), (0, [4]), (7, list(range(5, 75)))):
+        ref, S = d[where].double().sum(0), d[where].double().abs().sum(0)
+        assert ((grad[v].double() - ref).abs() <= (len(where) + 1) * 2.0 ** -24 * S).all()
+    named = torch.zeros(37, dtype=torch.bool, device="cuda")
+    named[[4, 36, 0, 7]] = True
+    assert (grad[~named] == 0).all()
+
+
+@pytest.mark.gpu
+def test_one_token_at_every_position(ssb):
+    """The longest run: every position names one id, beside positions that name none."""
+    T, H = 1 << 20, 8
+    d = torch.randint(-8, 9, (T, H), device="cuda").to(BF16)  # sums of integers: exact below 2^24
+    tokens = torch.full((T,), 99, dtype=torch.int32, device="cuda")
+    tokens[::1000] = -1
+    out = ssb.embed_grad(d, tokens, 100)
+    ref = d[tokens == 99].double().sum(0)
+    assert torch.equal(out[99].double(), ref) and (out[:99] == 0).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [3, 40])
 def test_head_takes_float32_whole(ssb, T):
     """Hidden states that differ beyond bfloat16: the result keeps what float32 has.  A table row of a single one
