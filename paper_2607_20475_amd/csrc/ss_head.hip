@@ -646,6 +646,13 @@ static void launch_few(HeadArgs& a, int cus, hipStream_t st) {
     hipLaunchKernelGGL((ss_head_few_kernel<KIND, DT, true>), grid, block, 0, st, a);
 }
 
+// Whether up to 16 float32 rows are split by every workgroup for itself, not by a launch of 4 us before the product.  T = 8, us, split on
+// the way / before (that launch apart): V = 32768, H = 2048 int128 15 / 13, int32 16 / 14, mx 15 / 12; V = 65536, H = 4096 49 / 38, 61 / 41,
+// 43 / 43; V = 212992, H = 4352 157 / 131, 203 / 145, 151 / 141.
+static bool small_for_split(const HeadArgs& a, int kind, int cus) {
+  return (int64_t)((a.V + 15) / 16) * a.nb < (int64_t)(kind == kMx ? 1024 : 256) * cus;
+}
+
 // direct: the hidden rows as the caller has them, else their parts or their copy.  V = 32768, H = 2048, T = 32: tiles (NV, CB, WAVES)
 // (2, 1, 8) 30 us, (1, 2, 8) 20; V = 131072, H = 4096: 112 and 144.
 template <int KIND>
@@ -753,11 +760,11 @@ ss_status ss_head_w4(const void* h, int dtype, int T, int64_t ld_h, const ss_w4*
   a.H = t->H;
   a.nb = w4_blocks(t->H);
   a.out_f32 = out_dtype == SS_F32;
-  // few float32 rows are split by the product's own loads, more of them once, before it
+  // float32 rows are split by the product's own loads where they and the table are few, else once, before it
   const int cus = compute_units();
   if (cus <= 0) return SS_ERR_HIP;
   const bool few = T <= (dtype == SS_F32 ? 4 : 16) && few_pays(a, cus);  // reads rows at any address
-  const bool direct = few || (wide_rows(h, ld_h, dtype) && (dtype == SS_BF16 || T <= 16));
+  const bool direct = few || (wide_rows(h, ld_h, dtype) && (dtype == SS_BF16 || (T <= 16 && small_for_split(a, kind, cus))));
   if (direct) {
     a.h = h;
     a.ld_h = ld_h;
