@@ -106,6 +106,7 @@ struct GradArgs {
   int wide_in, wide_out, accumulate;
   uint32_t blocks;                     // workgroups that have something to do
   uint32_t tiles, wtiles, cuts, heads;  // column tiles, one and kWide; cuts of the list; groups of kHeads entries
+  uint32_t strips;                     // waves' pieces of 1 KB of a row
 };
 
 __global__ __launch_bounds__(kSortThreads) void ss_grad_sort_kernel(GradArgs a) {
@@ -335,7 +336,8 @@ __device__ __forceinline__ void sum_part(const GradArgs& a, int p0, int p1, int 
 //           its first entry (piece 0) and one that begins later and leaves it (piece 1).
 //   runs    the rows of the short runs that begin among kHeads entries.  The list, not the table, is
 //           shared out: wherever its rows lie, the runs go to all parts of the chip.
-//   zeros   the rows without a run, in the order of memory, kPieces pieces of 4 KB to a workgroup (none when accumulating).
+//   zeros   the rows without a run, in the order of memory, kPieces pieces of 1 KB to a wave (none when accumulating).  V = 112616,
+//           H = 2816, float32, T = 97: 230 us (5.5 TB/s; pieces of 4 KB to a workgroup, the row's last not full: 248).
 // The first two start first, the zeros' stores follow: dealt out in turn with them, loads and stores that lie apart slow
 // the stores in order down.  At 16384 tokens by Zipf's law, bfloat16 to float32, V = 131072, H = 4096 (2.27 GB): 452 us with sort and join;
 // dealt out in turn 583; 1, 2, 4 and 8 pieces 642, 549, 538 and 587 (with the runs' rows among the zeros'); runs up to 16, 32 and
@@ -377,16 +379,17 @@ __global__ __launch_bounds__(256) void ss_grad_rows_kernel(GradArgs a) {
   }
   b -= a.heads * a.wtiles;
   const float zero[N] = {};
+  const uint32_t first = b * (4 * kPieces) + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t v[kPieces];
   bool none[kPieces];
 #pragma unroll
   for (int k = 0; k < kPieces; ++k) {
-    v[k] = (b * kPieces + k) / a.tiles;
+    v[k] = (first + 4 * k) / a.strips;
     none[k] = v[k] < (uint32_t)a.V && a.start[v[k]] == a.start[v[k] + 1];
   }
 #pragma unroll
   for (int k = 0; k < kPieces; ++k) {
-    const int col = (int)(b * kPieces + k - v[k] * a.tiles) * TILE + (int)threadIdx.x * N;
+    const int col = (int)(first + 4 * k - v[k] * a.strips) * (64 * N) + (int)(threadIdx.x & 63) * N;
     if (none[k]) cols_store<ODT, N>(a.out, (int64_t)v[k] * a.ld_out + col, a.H - col, a.wide_out, zero);
   }
 }
@@ -457,10 +460,14 @@ static bool grad_layout(int T, int V, int H, GradLayout* l) {
 template <int DT, int ODT>
 static void launch_sums(GradArgs& a, hipStream_t st) {
   a.tiles = (uint32_t)((a.H + Cols<ODT>::kTile - 1) / Cols<ODT>::kTile);
+  // whole rows of a workgroup's four waves rather than three pieces a row: V = 182836, H = 1280, bfloat16 96 us against 86 (two
+  // pieces stay two: V = 300000, H = 640 76 against 145 in fours)
+  a.strips = (uint32_t)((a.H + 64 * Cols<ODT>::N - 1) / (64 * Cols<ODT>::N));
+  if (a.strips == 3) a.strips = 4;
   a.cuts = a.T > kRun ? (uint32_t)((a.T + kRun - 1) / kRun) : 0u;
   a.heads = (uint32_t)((a.T + kHeads - 1) / kHeads);
   a.wtiles = (a.tiles + kWide - 1) / kWide;
-  const uint32_t zeros = a.accumulate ? 0u : ((uint32_t)a.V * a.tiles + kPieces - 1) / kPieces, most = 1u << 16;
+  const uint32_t zeros = a.accumulate ? 0u : ((uint32_t)a.V * a.strips + 4 * kPieces - 1) / (4 * kPieces), most = 1u << 16;
   a.blocks = a.cuts * a.tiles + a.heads * a.wtiles + zeros;
   if (a.blocks == 0) return;
   // in rows of 2^16: a launch has fewer than 2^32 threads in one direction
