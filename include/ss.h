@@ -42,7 +42,9 @@
  *     conditions never stop the call: they are reported per row in `flags`.
  *   - Launch shapes depend only on (B, V, L, k_max, dtype): every call can be
  *     captured in a HIP graph.  Per-call values (seed, position, params) are
- *     read from device memory.
+ *     read from device memory.  (The vocabulary operators': on sizes, types,
+ *     strides and alignment, never on tokens; their `scale` is a host value, which a
+ *     captured call keeps.)
  *   - The workspace needs no initialisation: every call writes what it reads
  *     (its contents between calls are unspecified), so one workspace of the
  *     largest size may serve calls of any operation and shape.  Calls that
