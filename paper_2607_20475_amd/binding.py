@@ -501,8 +501,11 @@ def _tokens(tokens, dev):
 
 
 def _table(table, dev):
-    if table.codes.get_device() != dev:
-        _elsewhere(table.codes, "table")
+    codes = table._codes
+    if codes.get_device() != dev:
+        _elsewhere(codes, "table")
+    if (codes.data_ptr(), table._scales.data_ptr()) != table._at:
+        raise SSError("the table's arrays have moved: make a new W4 of them")
 
 
 def _space(ws, dev):
@@ -522,7 +525,8 @@ def _device():
 class W4:
     """A vocabulary table in 4 bits (``ss_w4`` in ss.h): codes uint8 [V, 64 ceil(H / 128)] and scales
     [V, ceil(H / 128) 128 / group], bfloat16 for ``fmt`` "int" (groups of 32, 64 or 128 columns) and
-    uint8 for "mx" (groups of 32)."""
+    uint8 for "mx" (groups of 32).  Its sizes and arrays stay those it was made with: what the arrays hold may change,
+    and a table of other arrays is another W4."""
 
     FMT = {"int": W4_INT, "mx": W4_MX}
 
@@ -535,11 +539,20 @@ class W4:
             raise SSError(f"scales must be contiguous {dt} [{V}, {nb * 128 // group}]")
         if codes.device != scales.device:
             raise SSError("codes and scales are on different devices")
-        self.V, self.H, self.fmt, self.group = int(V), int(H), fmt, int(group)
-        self.codes, self.scales = codes, scales
-        st.codes, st.scales = codes.data_ptr(), scales.data_ptr()
+        self._V, self._H, self._fmt, self._group = int(V), int(H), fmt, int(group)
+        self._codes, self._scales = codes, scales
+        self._at = codes.data_ptr(), scales.data_ptr()
+        st.codes, st.scales = self._at
         self._struct = st
         self._ref = C.addressof(st)
+
+    # read-only: calls pass the struct, which was made from them
+    V = property(lambda self: self._V)
+    H = property(lambda self: self._H)
+    fmt = property(lambda self: self._fmt)
+    group = property(lambda self: self._group)
+    codes = property(lambda self: self._codes)
+    scales = property(lambda self: self._scales)
 
     @staticmethod
     def _sizes(V, H, fmt, group):
@@ -563,11 +576,11 @@ def quantize_w4(w, table=None, fmt="int", group=128, values=None):
     """The 4-bit form of w [V, H] (bfloat16 or float32), written to ``table`` (a new one of ``fmt`` and ``group`` if
     None) and returned; ``values`` [V, H], if given, gets the numbers that the codes stand for."""
     dev = _device()
-    ld, dt = _rows(w, "w", dev, *(() if table is None else (table.V, table.H)))
+    ld, dt = _rows(w, "w", dev, *(() if table is None else (table._V, table._H)))
     if table is None:
         table = W4.empty(w.shape[0], w.shape[1], fmt, group, w.device)
     _table(table, dev)
-    vld, vdt = (0, F32) if values is None else _rows(values, "values", dev, table.V, table.H)
+    vld, vdt = (0, F32) if values is None else _rows(values, "values", dev, table._V, table._H)
     _check(lib().ss_quant_w4(w.data_ptr(), dt, ld, table._ref, _ptr(values), vdt, vld, _raw(dev)))
     return table
 
@@ -583,12 +596,12 @@ def head_workspace(h):
 def head_w4(h, table, out=None, dtype=None, ws=None):
     """Logits [T, V] of hidden states h [T, H] under a 4-bit table; ``dtype`` (of a new ``out``): that of h."""
     dev = _device()
-    ld, dt = _rows(h, "h", dev, None, table.H)
+    ld, dt = _rows(h, "h", dev, None, table._H)
     _table(table, dev)
     T = h.shape[0]
     if out is None:
-        out = torch.empty(T, table.V, dtype=dtype or h.dtype, device=h.device)
-    old, odt = _rows(out, "out", dev, T, table.V, dtype)
+        out = torch.empty(T, table._V, dtype=dtype or h.dtype, device=h.device)
+    old, odt = _rows(out, "out", dev, T, table._V, dtype)
     if ws is None:
         ws = head_workspace(h)
     space, n = _space(ws, dev)
@@ -603,7 +616,7 @@ def embed(tokens, table, scale=1.0, out=None, dtype=None):
     T = _tokens(tokens, dev)
     w4 = isinstance(table, W4)
     if w4:
-        H = table.H
+        H = table._H
         _table(table, dev)
     else:
         ld, dt = _rows(table, "table", dev)

@@ -251,6 +251,27 @@ def test_wrappers_refuse_what_they_cannot_pass_on():
         b.embed_grad(torch.zeros(1, 6).expand(4, 6), torch.zeros(4, dtype=torch.int32), 10)
 
 
+def test_a_table_keeps_the_arrays_it_was_made_with():
+    """Calls pass the addresses that a table was made with: neither they nor its sizes can be changed under it, and an
+    array that has moved is refused (before its place is looked at by a kernel)."""
+    from paper_2607_20475_amd import binding as b
+    t = b.W4.empty(4, 256, "int", 128, device="cpu")
+    for name, value in [("codes", torch.zeros(4, 128, dtype=torch.uint8)), ("scales", torch.zeros(4, 2, dtype=BF16)),
+                        ("V", 5), ("H", 128), ("fmt", "mx"), ("group", 64)]:
+        with pytest.raises(AttributeError):
+            setattr(t, name, value)
+    b._table(t, -1)  # (a CPU tensor's device index)
+    t.codes.fill_(3)
+    b._table(t, -1)
+    t.codes.set_(torch.zeros(4, 128, dtype=torch.uint8))
+    with pytest.raises(b.SSError, match="moved"):
+        b._table(t, -1)
+    t = b.W4.empty(4, 256, "int", 128, device="cpu")
+    t.scales.set_(torch.zeros(4, 2, dtype=BF16))
+    with pytest.raises(b.SSError, match="moved"):
+        b._table(t, -1)
+
+
 # ---------------------------------------------------------------------------
 # On the GPU
 # ---------------------------------------------------------------------------
