@@ -465,6 +465,21 @@ def process_logits(logits, params, k_max, out_logits=None, out_probs=None, flags
 # The two ends of the vocabulary: hidden states to logits, tokens to hidden states
 # ---------------------------------------------------------------------------
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16}
+# no size of these calls is larger (SS_MAX_V, SS_MAX_T); beyond 32 bits one would reach the library as another
+_MOST = 1 << 20
+
+
+def _size(n, name):
+    """A whole number that the library's 32 bits hold (its own limits are checked there)."""
+    try:
+        whole = int(n)
+    except (TypeError, ValueError, OverflowError):
+        whole = None
+    if whole is None or whole != n:
+        raise SSError(f"{name} must be a whole number, got {n!r}")
+    if not -_MOST <= whole <= _MOST:
+        raise SSError(f"{name} = {n} is more than {_MOST}")
+    return whole
 
 
 def _rows(t, name, dev, rows=None, cols=None, dtype=None):
@@ -474,6 +489,8 @@ def _rows(t, name, dev, rows=None, cols=None, dtype=None):
     if len(shape) != 2:
         raise SSError(f"{name} must be a matrix, got {list(shape)}")
     R, n = shape
+    if R > _MOST or n > _MOST:
+        raise SSError(f"{name} has more than {_MOST} rows or columns: {list(shape)}")
     ld = stride[0]
     if (n > 1 and stride[1] != 1) or (R > 1 and ld < n):
         raise SSError(f"{name} must have rows with unit column stride")
@@ -497,6 +514,8 @@ def _tokens(tokens, dev):
         raise SSError("tokens must be contiguous int32 [T]")
     if tokens.get_device() != dev:
         _elsewhere(tokens, "tokens")
+    if tokens.shape[0] > _MOST:
+        raise SSError(f"more than {_MOST} tokens: {tokens.shape[0]}")
     return tokens.shape[0]
 
 
@@ -532,6 +551,7 @@ class W4:
 
     def __init__(self, codes, scales, V, H, fmt="int", group=128):
         st, nb = W4._sizes(V, H, fmt, group)
+        V, H, group = st.V, st.H, st.group
         if codes.dtype != torch.uint8 or not codes.is_contiguous() or codes.shape != (V, 64 * nb):
             raise SSError(f"codes must be contiguous uint8 [{V}, {64 * nb}]")
         dt = torch.uint8 if fmt == "mx" else torch.bfloat16
@@ -539,7 +559,7 @@ class W4:
             raise SSError(f"scales must be contiguous {dt} [{V}, {nb * 128 // group}]")
         if codes.device != scales.device:
             raise SSError("codes and scales are on different devices")
-        self._V, self._H, self._fmt, self._group = int(V), int(H), fmt, int(group)
+        self._V, self._H, self._fmt, self._group = V, H, fmt, group
         self._codes, self._scales = codes, scales
         self._at = codes.data_ptr(), scales.data_ptr()
         st.codes, st.scales = self._at
@@ -558,15 +578,16 @@ class W4:
     def _sizes(V, H, fmt, group):
         if fmt not in W4.FMT:
             raise SSError(f"format {fmt!r} is neither int nor mx")
-        st = _W4(V=int(V), H=int(H), fmt=W4.FMT[fmt], group=int(group))
+        st = _W4(V=_size(V, "V"), H=_size(H, "H"), fmt=W4.FMT[fmt], group=_size(group, "group"))
         if lib().ss_w4_codes_bytes(C.byref(st)) == 0:
             raise SSError(f"no {fmt} table of {V} rows, {H} columns and groups of {group}")
-        return st, (int(H) + 127) // 128
+        return st, (st.H + 127) // 128
 
     @classmethod
     def empty(cls, V, H, fmt="int", group=128, device="cuda"):
         """A table for ``quantize_w4`` to fill."""
-        nb = W4._sizes(V, H, fmt, group)[1]
+        st, nb = W4._sizes(V, H, fmt, group)
+        V, H, group = st.V, st.H, st.group
         return cls(torch.empty(V, 64 * nb, dtype=torch.uint8, device=device),
                    torch.empty(V, nb * 128 // group, dtype=torch.uint8 if fmt == "mx" else torch.bfloat16, device=device),
                    V, H, fmt, group)
@@ -587,7 +608,7 @@ def quantize_w4(w, table=None, fmt="int", group=128, values=None):
 
 def head_workspace(h):
     """A workspace for ``head_w4`` of hidden states h (or any with as many or fewer rows)."""
-    n = int(lib().ss_head_w4_bytes(h.shape[0], h.shape[1], _dtype_code(h)))
+    n = int(lib().ss_head_w4_bytes(_size(h.shape[0], "rows of h"), _size(h.shape[1], "columns of h"), _dtype_code(h)))
     if n == 0:
         raise SSError("invalid sizes for workspace")
     return torch.empty(n, dtype=torch.uint8, device=h.device)
@@ -635,7 +656,7 @@ def embed(tokens, table, scale=1.0, out=None, dtype=None):
 
 def embed_grad_workspace(T, V, H, device="cuda"):
     """A workspace for ``embed_grad`` of these sizes."""
-    n = int(lib().ss_embed_grad_bytes(T, V, H))
+    n = int(lib().ss_embed_grad_bytes(_size(T, "T"), _size(V, "V"), _size(H, "H")))
     if n == 0:
         raise SSError("invalid sizes for workspace")
     return torch.empty(n, dtype=torch.uint8, device=device)
@@ -645,6 +666,7 @@ def embed_grad(dout, tokens, V, scale=1.0, out=None, dtype=torch.float32, accumu
     """The table's gradient [V, H] of ``embed``: scale * the sum of dout [T, H] over each token's positions.
     ``accumulate`` adds it to ``out`` and leaves the rows that no token names as they were."""
     dev = _device()
+    V = _size(V, "V")
     ld, dt = _rows(dout, "dout", dev)
     T, H = dout.shape
     if _tokens(tokens, dev) != T:

@@ -272,6 +272,37 @@ def test_a_table_keeps_the_arrays_it_was_made_with():
         b._table(t, -1)
 
 
+def test_sizes_reach_the_library_as_they_are():
+    """Sizes that 32 bits do not hold, or that are no whole numbers, are refused: cut to 32 bits or to whole numbers
+    they would name other tables, with fewer rows or scales than the kernels read."""
+    from paper_2607_20475_amd import binding as b
+    wrap = 1 << 32
+    codes, scales = torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(4, 4, dtype=BF16)
+    for V, H, group in [(4 + wrap, 128, 32), (4, 128 + wrap, 32), (4, 128, 32 + wrap), (4, 128, 32 - wrap), (4, 128, 32.5),
+                        (4.5, 128, 32), (4, 128.25, 32), ("4", 128, 32), (None, 128, 32), (float("nan"), 128, 32)]:
+        with pytest.raises(b.SSError):
+            b.W4.empty(V, H, "int", group, device="cpu")
+        with pytest.raises(b.SSError):
+            b.W4(codes, scales, V, H, "int", group)
+    with pytest.raises(b.SSError):
+        b.W4(codes, scales[:, :3].contiguous(), 4, 128, "int", 32.5)
+    t = b.W4(codes, scales, np.int64(4), np.int64(128), "int", np.int64(32))
+    assert (t._struct.V, t._struct.H, t._struct.group) == (t.V, t.H, t.group) == (4, 128, 32)
+    for T, V, H in [(5 + wrap, 10, 8), (5, 10 + wrap, 8), (5, 10, 8 + wrap), (5, 10.5, 8)]:
+        with pytest.raises(b.SSError):
+            b.embed_grad_workspace(T, V, H, device="cpu")
+    with pytest.raises(b.SSError, match="V = "):
+        b.embed_grad(torch.zeros(2, 8), torch.zeros(2, dtype=torch.int32), 10 + wrap)
+    # rows beyond 2^32, without their memory: a view of one row
+    tall = torch.zeros(1, 32, dtype=BF16).expand(wrap + 4, 32)
+    with pytest.raises(b.SSError, match="more than"):
+        b._rows(tall, "table", -1)
+    with pytest.raises(b.SSError, match="more than"):
+        b._tokens(torch.empty(wrap + 4, dtype=torch.int32, device="meta"), -1)
+    with pytest.raises(b.SSError):
+        b.head_workspace(tall)
+
+
 # ---------------------------------------------------------------------------
 # On the GPU
 # ---------------------------------------------------------------------------
