@@ -531,6 +531,8 @@ def _space(ws, dev):
     """(pointer, bytes) of a workspace."""
     if ws.get_device() != dev:
         _elsewhere(ws, "ws")
+    if not ws.is_contiguous():
+        raise SSError("ws must be contiguous: its bytes are used from the first on")
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 

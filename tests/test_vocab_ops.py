@@ -303,6 +303,17 @@ def test_sizes_reach_the_library_as_they_are():
         b.head_workspace(tall)
 
 
+def test_a_workspace_has_the_bytes_that_it_is_taken_for():
+    """Elements times their size is the room behind the pointer only where they follow one another."""
+    from paper_2607_20475_amd import binding as b
+    ws = torch.zeros(64, 32, dtype=torch.int32)
+    assert b._space(ws, -1) == (ws.data_ptr(), 64 * 32 * 4)
+    assert b._space(ws[8:], -1) == (ws.data_ptr() + 8 * 32 * 4, 56 * 32 * 4)
+    for bad in (ws[:1, :1].expand(64, 1024), ws[:, ::2], ws.t(), ws[:, :16]):
+        with pytest.raises(b.SSError, match="contiguous"):
+            b._space(bad, -1)
+
+
 # ---------------------------------------------------------------------------
 # On the GPU
 # ---------------------------------------------------------------------------
