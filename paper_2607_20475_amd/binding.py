@@ -595,9 +595,15 @@ class W4:
                    V, H, fmt, group)
 
 
-def quantize_w4(w, table=None, fmt="int", group=128, values=None):
-    """The 4-bit form of w [V, H] (bfloat16 or float32), written to ``table`` (a new one of ``fmt`` and ``group`` if
-    None) and returned; ``values`` [V, H], if given, gets the numbers that the codes stand for."""
+def quantize_w4(w, table=None, fmt=None, group=None, values=None):
+    """The 4-bit form of w [V, H] (bfloat16 or float32), written to ``table`` (None: a new one of ``fmt``, "int" unless
+    given, and ``group``, 128 unless given) and returned; ``values`` [V, H], if given, gets the numbers that the codes
+    stand for."""
+    if table is None:
+        fmt, group = "int" if fmt is None else fmt, 128 if group is None else group
+    elif fmt not in (None, table._fmt) or group not in (None, table._group):
+        raise SSError(f"table is {table._fmt} in groups of {table._group}, not {fmt or table._fmt} in groups of "
+                      f"{table._group if group is None else group}")
     dev = _device()
     ld, dt = _rows(w, "w", dev, *(() if table is None else (table._V, table._H)))
     if table is None:
@@ -664,8 +670,9 @@ def embed_grad_workspace(T, V, H, device="cuda"):
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def embed_grad(dout, tokens, V, scale=1.0, out=None, dtype=torch.float32, accumulate=False, ws=None):
+def embed_grad(dout, tokens, V, scale=1.0, out=None, dtype=None, accumulate=False, ws=None):
     """The table's gradient [V, H] of ``embed``: scale * the sum of dout [T, H] over each token's positions.
+    ``dtype`` (of a new ``out``): float32 unless given.
     ``accumulate`` adds it to ``out`` and leaves the rows that no token names as they were."""
     dev = _device()
     V = _size(V, "V")
@@ -676,8 +683,8 @@ def embed_grad(dout, tokens, V, scale=1.0, out=None, dtype=torch.float32, accumu
     if out is None:
         if accumulate:
             raise SSError("accumulate needs out")
-        out = torch.empty(V, H, dtype=dtype, device=dout.device)
-    old, odt = _rows(out, "out", dev, V, H)
+        out = torch.empty(V, H, dtype=dtype or torch.float32, device=dout.device)
+    old, odt = _rows(out, "out", dev, V, H, dtype)
     if ws is None:
         ws = embed_grad_workspace(T, V, H, dout.device)
     space, n = _space(ws, dev)

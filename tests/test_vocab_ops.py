@@ -314,6 +314,30 @@ def test_a_workspace_has_the_bytes_that_it_is_taken_for():
             b._space(bad, -1)
 
 
+def test_what_a_call_asks_for_is_not_passed_over():
+    """A format, group or type that differs from the table or output that is handed in."""
+    from paper_2607_20475_amd import binding as b
+    t = b.W4.empty(4, 256, "mx", 32, device="cpu")
+    w = torch.zeros(4, 256)
+    for bad in (dict(fmt="int"), dict(group=64), dict(fmt="mx", group=128)):
+        with pytest.raises(b.SSError, match="table is mx in groups of 32"):
+            b.quantize_w4(w, t, **bad)
+    for good in (dict(), dict(fmt="mx"), dict(group=32), dict(fmt="mx", group=32)):
+        with pytest.raises(b.SSError, match="not on a GPU"):
+            b.quantize_w4(w, t, **good)
+
+
+@pytest.mark.gpu
+def test_the_type_of_a_gradient_is_not_passed_over(ssb):
+    d, tok = torch.ones(3, 8, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    out = torch.zeros(2, 8, dtype=BF16, device="cuda")
+    with pytest.raises(ssb.SSError, match="out must be"):
+        ssb.embed_grad(d, tok, 2, out=out, dtype=F32)
+    assert ssb.embed_grad(d, tok, 2, out=out, dtype=BF16) is out and (out[0] == 3).all()
+    assert (ssb.embed_grad(d, tok, 2, out=out, accumulate=True)[0] == 6).all()
+    assert ssb.embed_grad(d, tok, 2).dtype == F32 and ssb.quantize_w4(torch.ones(2, 128, device="cuda")).group == 128
+
+
 # ---------------------------------------------------------------------------
 # On the GPU
 # ---------------------------------------------------------------------------
