@@ -478,6 +478,84 @@ def test_head_of_large_tables_with_more_rows(ssb, fmt, group, dtype, T):
         assert (out[:, V:] == 77).all()
 
 
+FORMS = [
+    # float32 hidden states?, T, V, H: every form of the head's kernels, and both sides of the rules between them.  More than
+    # 16 rows: four tiles of table rows a wave (and their last columns apart), two, one; workgroups of 16, 14 and 12 waves
+    (0, 64, 131072, 608), (0, 64, 131065, 608), (0, 320, 131072, 608), (0, 41, 131072, 608), (0, 41, 131065, 608),
+    (0, 32, 131072, 608), (0, 20, 131065, 608), (0, 20, 12301, 608), (0, 29, 161103, 608), (0, 29, 95003, 608),
+    (0, 64, 65521, 608), (0, 64, 161103, 608), (0, 64, 95003, 608),
+    # up to 16 rows: short rows, a table row more than the other kernel's first round, columns that fit LDS and that do not
+    (0, 16, 131077, 384), (0, 16, 131077, 512), (0, 9, 32768, 4096), (0, 9, 32769, 4096), (0, 16, 131072, 1056),
+    (0, 1, 131077, 1024), (0, 8, 16384, 8192), (0, 16, 16384, 8192), (0, 16, 40003, 6144), (0, 11, 4097, 608), (0, 3, 33001, 608),
+    # float32 hidden states
+    (1, 4, 131077, 1024), (1, 4, 33003, 6144), (1, 11, 131077, 672), (1, 9, 257, 96), (1, 9, 257, 640), (1, 20, 257, 640),
+    (1, 33, 40003, 160),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", KINDS)
+@pytest.mark.parametrize("part", range(4))
+def test_every_form_of_the_head(ssb, fmt, group, part):
+    """bfloat16 and float32 logits, rows of hidden states and logits at aligned and at odd addresses, against 64 bits."""
+    g = torch.Generator(device="cuda")
+    for f32, T, V, H in FORMS[part::4]:
+        H = (H + group - 1) // group * group
+        g.manual_seed(T + V + H)
+        nb = (H + 127) // 128
+        codes = torch.randint(0, 256, (V, 64 * nb), dtype=torch.uint8, device="cuda", generator=g)
+        if fmt == "mx":
+            scales = torch.randint(115, 125, (V, nb * 4), dtype=torch.uint8, device="cuda", generator=g)
+            scales[:, H // 32:] = 255
+        else:
+            scales = torch.empty(V, nb * 128 // group, device="cuda").uniform_(0.001, 0.02, generator=g).to(BF16)
+            scales[:, H // group:] = float("nan")
+        table = ssb.W4(codes, scales, V, H, fmt, group)
+        h = torch.empty(T, H, device="cuda").normal_(generator=g).to(F32 if f32 else BF16)
+        W = ssb.embed(torch.arange(V, dtype=torch.int32, device="cuda"), table, dtype=F32)
+        h64 = h.double()
+        ref, S = torch.empty(T, V, dtype=torch.float64, device="cuda"), torch.empty(T, V, dtype=torch.float64, device="cuda")
+        for r in range(0, V, 32768):
+            w = W[r:r + 32768].double()
+            ref[:, r:r + 32768], S[:, r:r + 32768] = h64 @ w.T, h64.abs() @ w.abs().T
+        slack = (32 + (3 if f32 else 1) * H / 32 + 24) * 2.0 ** -23 * S
+        for extra, shift in ((0, 0), (3, 1)):
+            hs, _ = strided(h, extra, shift)
+            for out_dtype in (BF16, F32):
+                say(f"[forms] {fmt}{group} {h.dtype} T={T} V={V} H={H} out={out_dtype} extra={extra}")
+                base = torch.full((T * (V + extra) + shift + 8,), 77.0, dtype=out_dtype, device="cuda")
+                rows = base[shift:shift + T * (V + extra)].view(T, V + extra)
+                ssb.head_w4(hs, table, out=rows[:, :V])
+                tol = slack * (1 + U[out_dtype]) + U[out_dtype] * ref.abs()
+                assert ((rows[:, :V].double() - ref).abs() <= tol).all()
+                assert (rows[:, V:] == 77).all() and (base[:shift] == 77).all() and (base[shift + T * (V + extra):] == 77).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", [("mx", 32), ("int", 128)])
+def test_rows_beyond_32_bits_bit_for_bit(ssb, fmt, group):
+    """A table of 4.5 GB against tables of some of its rows.  Sums of multiples of a half below 2^18: exact in any order."""
+    g = torch.Generator(device="cuda").manual_seed(16)
+    V, H = 1 << 20, 8704
+    nb = H // 128
+    codes = torch.empty(V, 64 * nb, dtype=torch.uint8, device="cuda")
+    for r in range(0, V, 1 << 17):
+        codes[r:r + (1 << 17)] = torch.randint(0, 256, (1 << 17, 64 * nb), dtype=torch.uint8, device="cuda", generator=g)
+    scales = (torch.full((V, nb * 4), 127, dtype=torch.uint8, device="cuda") if fmt == "mx"
+              else torch.ones(V, nb, dtype=BF16, device="cuda"))
+    big = ssb.W4(codes, scales, V, H, fmt, group)
+    at = [slice(0, 100), slice(493440, 493600), slice(986800, 987000), slice(V - 100, V)]  # 2^32 bytes lie at row 986895
+    few = [ssb.W4(codes[s].clone(), scales[s].clone(), s.stop - s.start, H, fmt, group) for s in at]
+    for dtype, T in ((BF16, 2), (BF16, 20), (BF16, 64), (F32, 2), (F32, 20)):
+        say(f"[4 GB exact] {fmt}{group} {dtype} T={T}")
+        h = torch.randint(-4, 5, (T, H), device="cuda", generator=g).to(dtype)
+        out = ssb.head_w4(h, big, dtype=F32)
+        for s, t in zip(at, few):
+            W = ssb.embed(torch.arange(t.V, dtype=torch.int32, device="cuda"), t, dtype=F32)
+            want = h.double() @ W.double().T
+            assert torch.equal(out[:, s].double(), want) and torch.equal(ssb.head_w4(h, t, dtype=F32), out[:, s])
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt,group", KINDS)
 def test_the_widest_rows(ssb, fmt, group):
