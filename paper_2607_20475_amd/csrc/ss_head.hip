@@ -623,11 +623,25 @@ static int compute_units() {
   return n;
 }
 
-// Whether a table is large enough for ss_head_few_kernel: two units at least for each of its waves.  What it starts with
-// (hidden rows to LDS) and ends with (the last units of all waves at once, sums of split tiles) takes 7 us against
-// 2 of the other kernel, whose rate is lower: 33 MB (V = 32768, H = 2048, T = 1) 14.5 us against 9.7, 67 MB 17 against 18.
-static bool few_pays(const HeadArgs& a, int cus) {
-  return (int64_t)((a.V + 15) / 16) * ((a.nb + kUnit - 1) / kUnit) >= (int64_t)2 * kFewWaves * cus;
+// Whether ss_head_few_kernel takes a call of up to 16 bfloat16 or 4 float32 rows.  It has more to start with (hidden rows to LDS) and to
+// end with (the last units of all waves at once, sums of split tiles) than the other kernel, and a higher rate.  Times: us, this
+// kernel / the other, int128, tables that no cache holds.
+//   Size: two units at least for each of its waves, a row's last, partial unit counted as one, as it is loaded.  T = 1: V = 32768, H = 2048
+//     (half of that) 13.0 / 10.8, V = 49152 16.9 / 17.5, V = 65536 18.0 / 18.5, V = 131072, H = 1024 18.0 / 22.0.
+// Against four float32 rows, three products each, the other kernel has nothing beyond that: 0.6 to 0.95 of its time, and the same
+// for rows of one or two blocks.  Against bfloat16 rows it has two things:
+//   Rows of fewer than four blocks: a unit is loaded whole.  T = 16: V = 131077, H = 128 12.0 / 7.0; V = 400000, H = 256 35 / 23, H = 384
+//     31 / 26, H = 512 41 / 49.  (Half-empty second units, H = 1536: 1.00 to 1.12 of the other's time.)
+//   At most one of its workgroups to a compute unit (8 tiles): one round, without a rest.  T = 16: V = 32768, H = 4096 21.3 / 17.4, V = 36869
+//     25.4 / 29.4; where the rows do not fit LDS, a wave takes whole tiles and half of the waves have none: H = 8192, V = 16384 29 / 25, V =
+//     32000 42 / 36, V = 50000 60 / 61; H = 65536, V = 16384 230 / 167.  Long rows that do fit are shared out evenly: H = 8192, V = 16384, T = 8 21.6 / 24.1;
+//     H = 6144, V = 22533, T = 1 21.1 / 22.4, T = 8 23.8 / 23.2; H = 4096, V = 32768, T = 1 17.6 / 16.9.
+static bool few_pays(const HeadArgs& a, bool f32, int cus) {
+  const int64_t tiles = (a.V + 15) / 16, units = (a.nb + kUnit - 1) / kUnit;
+  if (tiles * units < (int64_t)2 * kFewWaves * cus) return false;
+  if (f32) return true;
+  if (a.nb < 4) return false;
+  return tiles > (int64_t)8 * cus || (a.nb >= 48 && units * kUnit * kBlockCols * a.T <= kSlabBytes / 2);
 }
 
 template <int KIND, int DT>
@@ -657,7 +671,7 @@ static bool small_for_split(const HeadArgs& a, int kind, int cus) {
 // (2, 1, 8) 30 us, (1, 2, 8) 20; V = 131072, H = 4096: 112 and 144.
 template <int KIND>
 static void launch_head_f32(HeadArgs& a, bool direct, int cus, hipStream_t st) {
-  if (a.T <= 4 && few_pays(a, cus)) return launch_few<KIND, SS_F32>(a, cus, st);
+  if (a.T <= 4 && few_pays(a, true, cus)) return launch_few<KIND, SS_F32>(a, cus, st);
   const bool columns = a.nb >= 2, small = (int64_t)((a.V + 15) / 16) * ((a.T + 31) / 32) <= (int64_t)8 * cus;
   if (direct && columns) return launch_one<KIND, kFromF32, 3, 1, 1, 2, 8>(a, st);
   if (direct) return launch_one<KIND, kFromF32, 3, 1, 1, 1, 8>(a, st);
@@ -705,7 +719,7 @@ static void launch_48(HeadArgs& a, int64_t work, int cus, hipStream_t st) {
 //   V = 65536, H = 4096   T = 32: (4, 8) 37, (2, 16) 33.  T = 64: (2, 8) 55, (2, 16) 40.
 template <int KIND>
 static void launch_head_bf16(HeadArgs& a, int cus, hipStream_t st) {
-  if (a.T <= 16 && few_pays(a, cus)) return launch_few<KIND, SS_BF16>(a, cus, st);
+  if (a.T <= 16 && few_pays(a, false, cus)) return launch_few<KIND, SS_BF16>(a, cus, st);
   const int tiles = (a.T + 15) / 16, blocks = (tiles + 3) / 4, mt = (tiles + blocks - 1) / blocks;
   const int64_t work = (int64_t)((a.V + 15) / 16) * ((tiles + mt - 1) / mt);  // tiles of vocabulary rows, for each token block
   if (a.nb < 4) {  // fewer blocks than a chunk
@@ -763,7 +777,7 @@ ss_status ss_head_w4(const void* h, int dtype, int T, int64_t ld_h, const ss_w4*
   // float32 rows are split by the product's own loads where they and the table are few, else once, before it
   const int cus = compute_units();
   if (cus <= 0) return SS_ERR_HIP;
-  const bool few = T <= (dtype == SS_F32 ? 4 : 16) && few_pays(a, cus);  // reads rows at any address
+  const bool few = T <= (dtype == SS_F32 ? 4 : 16) && few_pays(a, dtype == SS_F32, cus);  // reads rows at any address
   const bool direct = few || (wide_rows(h, ld_h, dtype) && (dtype == SS_BF16 || (T <= 16 && small_for_split(a, kind, cus))));
   if (direct) {
     a.h = h;
