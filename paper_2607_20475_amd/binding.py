@@ -144,9 +144,12 @@ def _stream():
     return _raw_stream(torch.cuda.current_device())
 
 
-def _raw(dev):
-    """The current stream of device `dev`, the current one."""
-    return _stream() if _raw_stream is None else _raw_stream(dev)
+def _any_stream(dev):
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+# the current stream of a device
+_raw = _raw_stream or _any_stream
 
 
 def _dtype_code(t):
@@ -489,8 +492,8 @@ def _rows(t, name, dev, rows=None, cols=None, dtype=None):
     if len(shape) != 2:
         raise SSError(f"{name} must be a matrix, got {list(shape)}")
     R, n = shape
-    if R > _MOST or n > _MOST:
-        raise SSError(f"{name} has more than {_MOST} rows or columns: {list(shape)}")
+    if (R | n) > 0x7FFFFFFF:
+        raise SSError(f"{name} has more rows or columns than 32 bits hold: {list(shape)}")
     ld = stride[0]
     if (n > 1 and stride[1] != 1) or (R > 1 and ld < n):
         raise SSError(f"{name} must have rows with unit column stride")
@@ -514,16 +517,18 @@ def _tokens(tokens, dev):
         raise SSError("tokens must be contiguous int32 [T]")
     if tokens.get_device() != dev:
         _elsewhere(tokens, "tokens")
-    if tokens.shape[0] > _MOST:
-        raise SSError(f"more than {_MOST} tokens: {tokens.shape[0]}")
-    return tokens.shape[0]
+    T = tokens.shape[0]
+    if T > 0x7FFFFFFF:
+        raise SSError(f"more tokens than 32 bits hold: {T}")
+    return T
 
 
 def _table(table, dev):
     codes = table._codes
     if codes.get_device() != dev:
         _elsewhere(codes, "table")
-    if (codes.data_ptr(), table._scales.data_ptr()) != table._at:
+    at = table._at
+    if codes.data_ptr() != at[0] or table._scales.data_ptr() != at[1]:
         raise SSError("the table's arrays have moved: make a new W4 of them")
 
 
@@ -610,7 +615,9 @@ def quantize_w4(w, table=None, fmt=None, group=None, values=None):
         table = W4.empty(w.shape[0], w.shape[1], fmt, group, w.device)
     _table(table, dev)
     vld, vdt = (0, F32) if values is None else _rows(values, "values", dev, table._V, table._H)
-    _check(lib().ss_quant_w4(w.data_ptr(), dt, ld, table._ref, _ptr(values), vdt, vld, _raw(dev)))
+    st = (_lib or lib()).ss_quant_w4(w.data_ptr(), dt, ld, table._ref, _ptr(values), vdt, vld, _raw(dev))
+    if st:
+        _check(st)
     return table
 
 
@@ -634,7 +641,9 @@ def head_w4(h, table, out=None, dtype=None, ws=None):
     if ws is None:
         ws = head_workspace(h)
     space, n = _space(ws, dev)
-    _check(lib().ss_head_w4(h.data_ptr(), dt, T, ld, table._ref, out.data_ptr(), odt, old, space, n, _raw(dev)))
+    st = (_lib or lib()).ss_head_w4(h.data_ptr(), dt, T, ld, table._ref, out.data_ptr(), odt, old, space, n, _raw(dev))
+    if st:
+        _check(st)
     return out
 
 
@@ -654,11 +663,12 @@ def embed(tokens, table, scale=1.0, out=None, dtype=None):
         out = torch.empty(T, H, dtype=dtype or (torch.bfloat16 if w4 else table.dtype), device=tokens.device)
     old, odt = _rows(out, "out", dev, T, H, dtype)
     if w4:
-        st = lib().ss_embed_w4(tokens.data_ptr(), T, table._ref, scale, out.data_ptr(), odt, old, _raw(dev))
+        st = (_lib or lib()).ss_embed_w4(tokens.data_ptr(), T, table._ref, scale, out.data_ptr(), odt, old, _raw(dev))
     else:
-        st = lib().ss_embed(tokens.data_ptr(), T, table.data_ptr(), dt, V, H, ld, scale, out.data_ptr(), odt, old,
-                            _raw(dev))
-    _check(st)
+        st = (_lib or lib()).ss_embed(tokens.data_ptr(), T, table.data_ptr(), dt, V, H, ld, scale, out.data_ptr(), odt,
+                                      old, _raw(dev))
+    if st:
+        _check(st)
     return out
 
 
@@ -688,8 +698,10 @@ def embed_grad(dout, tokens, V, scale=1.0, out=None, dtype=None, accumulate=Fals
     if ws is None:
         ws = embed_grad_workspace(T, V, H, dout.device)
     space, n = _space(ws, dev)
-    _check(lib().ss_embed_grad(dout.data_ptr(), dt, T, ld, tokens.data_ptr(), V, H, scale, out.data_ptr(), odt, old,
-                               accumulate, space, n, _raw(dev)))
+    st = (_lib or lib()).ss_embed_grad(dout.data_ptr(), dt, T, ld, tokens.data_ptr(), V, H, scale, out.data_ptr(), odt,
+                                       old, accumulate, space, n, _raw(dev))
+    if st:
+        _check(st)
     return out
 
 
