@@ -22,7 +22,8 @@
  *   ss_logprobs        top-k log-probabilities under the full-row distribution
  *                      (indicator bit 0x400, Section 3.5)
  * and the operators at the two ends of the vocabulary, which make the logits
- * that these read and take up the tokens that they give:
+ * that these read and take up the tokens that they give (what such a call writes
+ * overlaps no other array of the call, unless it says so):
  *   ss_head_w4         logits of hidden states under a 4-bit vocabulary table
  *   ss_embed, ss_embed_w4   rows of the vocabulary table by token
  *   ss_embed_grad      the gradient of such a lookup, by sorted tokens
@@ -30,9 +31,10 @@
  *
  * Conventions (all functions):
  *   - Every array argument is a DEVICE pointer owned by the caller, except
- *     `const ss_params*`, which is a host struct whose members are device
- *     pointers.  The library never allocates, frees or synchronises; every
- *     launch goes to `stream` (a hipStream_t, NULL = default stream).
+ *     `const ss_params*` and `const ss_w4*`, host structs whose members are device
+ *     pointers, read during the call.  The library never allocates, frees or
+ *     synchronises; every launch goes to `stream` (a hipStream_t, NULL = default
+ *     stream).
  *   - Row-major layouts with an explicit row stride `ld` (elements).
  *   - Per-request parameter arrays have B entries.  A NULL parameter array
  *     disables the indicator bits that need it (e.g. temperature == NULL
@@ -374,14 +376,16 @@ size_t ss_w4_scales_bytes(const ss_w4 *t);
  * scales that `t` points to, for each group of a row from its largest
  * magnitude a:
  *   SS_W4_INT  s = a / 7 rounded to float32 and then to bfloat16, code = w / s rounded
- *              to the nearest integer (ties to even) of -7..7; s = 0 gives codes 0.
+ *              to the nearest integer (ties to even) of -7..7; s = 0 gives magnitudes 0.
  *   SS_W4_MX   2^e with e = floor(log2 a) - 2, not below -127; code = w / 2^e
  *              rounded to the nearest E2M1 number (ties to the even code), at most 6.
- * Quotients are rounded once, as if exact.  A group that holds a NaN or an
- * infinity gets a NaN scale and codes 0.  Columns beyond H are filled with zeros.
+ * Quotients are rounded once, as if exact.  A code keeps its weight's sign, at magnitude 0 too.
+ * A group that holds a NaN or an infinity gets a NaN scale and codes 0 without signs.  Columns
+ * beyond H are filled with zeros.
  *   w       [V, ld] of `dtype`, ld >= H.
  *   values  NULL, or [V, ld_values] of `values_dtype`: the numbers that the codes stand for
- *           (code * scale, rounded once), as training against the quantised table needs.
+ *           (code * scale, rounded once), as training against the quantised table needs.  May be
+ *           w itself, with its type and stride.
  */
 ss_status ss_quant_w4(const void *w, int dtype, int64_t ld, const ss_w4 *t, void *values, int values_dtype,
                       int64_t ld_values, void *stream);

@@ -882,6 +882,21 @@ def test_quantiser_by_its_definition(ssb, fmt, group, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", KINDS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_values_written_over_the_weights(ssb, fmt, group, dtype):
+    """`values` may be the weights themselves: the table and the numbers of a call with another array."""
+    g = torch.Generator(device="cuda").manual_seed(17)
+    for V, H, extra in ((37, 160, 0), (50, 4096, 8), (9, 2944, 3)):
+        H = (H + group - 1) // group * group
+        w, _ = strided(torch.empty(V, H, dtype=dtype, device="cuda").normal_(0, 0.02, generator=g), extra)
+        apart = torch.empty(V, H, dtype=dtype, device="cuda")
+        want = ssb.quantize_w4(w, fmt=fmt, group=group, values=apart)
+        got = ssb.quantize_w4(w, fmt=fmt, group=group, values=w)
+        assert torch.equal(got.codes, want.codes) and torch.equal(got.scales, want.scales) and torch.equal(w, apart)
+
+
+@pytest.mark.gpu
 def test_wrappers_refuse_on_the_gpu(ssb):
     t = ssb.W4.empty(64, 256, "int", 128)
     h = torch.zeros(4, 256, dtype=BF16, device="cuda")
