@@ -8,9 +8,13 @@
 //   those below its range (where its part of the sorted list starts) and, per
 //   wave and id, those in it; the second scan puts each position in its
 //   place, in ascending order for each id.  No workgroup waits for another and no
-//   atomics decide an order.  The scan costs (V / range) * T * 8 bytes of L2 reads,
-//   against T * H * 2 or more of the sum and V * H * 2 or more of the result: 7 us at V =
-//   32768, T = 2048 (of 65 in all, H = 2048, float32), 19 at V = 131072, T = 16384 (of 452, below).
+//   atomics decide an order.  The scans read (V / range) * T * 4 bytes from L2, twice that
+//   above 16384 tokens, which a wave's registers do not hold from one to the other,
+//   against T * H * 2 or more of the sum and V * H * 2 or more of the result: 6 us at V =
+//   32768, T = 2048 (of 65 in all, H = 2048, float32), 19 at V = 131072, T = 16384 (of 455, below).
+//   When accumulating, only named rows are written, and the sort and the chain of three
+//   launches weigh more: 23 us at T = 2048 (985 rows of H = 2048 float32, 31 MB), 129 at T = 16384
+//   (6305 of H = 4096, 327 MB), 16 at T = 64, V = 131072.
 //   Sum.  A row whose run is short adds its rows of dout in order.  The list is cut at
 //   multiples of kRun; of a longer run, each cut's part is summed by a
 //   workgroup of its own and a last launch adds the parts in order (5 and 9 us).
@@ -338,10 +342,12 @@ __device__ __forceinline__ void sum_part(const GradArgs& a, int p0, int p1, int 
 //           shared out: wherever its rows lie, the runs go to all parts of the chip.
 //   zeros   the rows without a run, in the order of memory, kPieces pieces of 1 KB to a wave (none when accumulating).  V = 112616,
 //           H = 2816, float32, T = 97: 230 us (5.5 TB/s; pieces of 4 KB to a workgroup, the row's last not full: 248).
-// The first two start first, the zeros' stores follow: dealt out in turn with them, loads and stores that lie apart slow
-// the stores in order down.  At 16384 tokens by Zipf's law, bfloat16 to float32, V = 131072, H = 4096 (2.27 GB): 452 us with sort and join;
-// dealt out in turn 583; 1, 2, 4 and 8 pieces 642, 549, 538 and 587 (with the runs' rows among the zeros'); runs up to 16, 32 and
-// 64 entries short 456, 453 and 481; one entry a workgroup puts runs of equal lengths on few XCDs (2000 runs of 8: 648 against 464).
+// The first two start first, the zeros' stores follow: dealt out in turn with them, loads and stores that lie apart slow the
+// stores in order down (583 us at the following size).  16384 tokens by Zipf's law, bfloat16 to float32, V = 131072, H = 4096
+// (2.27 GB), with sort and join: 459 us; pieces 1, 2 and 8 618, 476 and 462
+// (the 112616 rows: 235 of 4, 285, 225 and 240); runs up to 16 and 64 entries short 458 and 457 (T = 2048, V =
+// 32768, H = 2048, float32: 68 of 32, 68 and 75; T = 16384, accumulating: 129 of 32, 122 and 152).  One entry a workgroup puts runs of
+// equal lengths on few XCDs (2000 runs of 8: 648 against 464).
 constexpr int kHeads = 3, kPieces = 4, kWide = 2;
 
 template <int DT, int ODT>
@@ -460,8 +466,8 @@ static bool grad_layout(int T, int V, int H, GradLayout* l) {
 template <int DT, int ODT>
 static void launch_sums(GradArgs& a, hipStream_t st) {
   a.tiles = (uint32_t)((a.H + Cols<ODT>::kTile - 1) / Cols<ODT>::kTile);
-  // whole rows of a workgroup's four waves rather than three pieces a row: V = 182836, H = 1280, bfloat16 96 us against 86 (two
-  // pieces stay two: V = 300000, H = 640 76 against 145 in fours)
+  // A row of three pieces is dealt out as four, the last one empty, so that a workgroup's four waves have a row: V = 182836, H =
+  // 1280, bfloat16, T = 1000 103 us against 110 in threes.  Two pieces stay two: V = 300000, H = 640, T = 97 80 us against 145 in fours.
   a.strips = (uint32_t)((a.H + 64 * Cols<ODT>::N - 1) / (64 * Cols<ODT>::N));
   if (a.strips == 3) a.strips = 4;
   a.cuts = a.T > kRun ? (uint32_t)((a.T + kRun - 1) / kRun) : 0u;

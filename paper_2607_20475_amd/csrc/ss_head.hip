@@ -392,10 +392,16 @@ enum HeadSource { kFromBf16 = 0, kFromF32 = 1 };
 
 // A workgroup has WAVES waves; each wave has NV tiles of 16 vocabulary rows and all MT tiles of 16 tokens, and takes CB blocks
 // of columns (a chunk) at a time, codes of the next chunk in flight.  Up to 16 tokens it is bound by the table's read and the
-// start of its workgroups (V = 32768, H = 2048, T = 1: 8.7 us, 4.0 TB/s), beyond by the issue of vector instructions: a step of
-// 32 columns takes 7 to expand the codes (4 for E2M1), 4 MT / (group / 32) to scale sums (none for E2M1) and a few for
-// addresses, beside MT matrix instructions of 16 cycles.  V = 131072, H = 4096: T = 64 int128 87 us, 790 TFLOP/s; T = 320 mx 342
-// us, 1000 TFLOP/s (a library's product of bfloat16 matrices of these sizes: 353 us); V = 200003, H = 2880, T = 37 int32: 117 us.
+// start of its workgroups (V = 32768, H = 2048, T = 1: 8.7 us, 4.0 TB/s).  Beyond, a step of 32 columns takes, for each tile of vocabulary
+// rows, 7 vector instructions to expand the codes (4 for E2M1), 4 MT / (group / 32) to scale sums (none for E2M1) and a few for
+// addresses, MT matrix instructions of 16 cycles, and MT / NV reads of 1 KB from LDS.  Shares of the kernel's cycles:
+//   T = 64 int128, V = 131072, H = 4096 (NV = 1)  88 to 92 us, 780 to 750 TFLOP/s: vector issue 48 %, LDS 46 %, matrix units 41 %;
+//     waves wait for issue 41 % of their time and for loads and barriers 41 %.
+//   T = 320 mx, the same table (NV = 4)  342 us, 1000 TFLOP/s: matrix units 41 %, vector issue 29 %, LDS 13 %.  (A library's product of
+//     bfloat16 matrices of these sizes: 353 us.)  int128 376 to 400, int32 457 to 473 with NV = 1.
+//   T = 37 int32, V = 200003, H = 2880  117 us: vector issue 48 %, LDS 27 %, matrix units 21 %.  A sum of 32 columns is scaled as soon as
+//     its products are there: the compiler puts 274 cycles of s_nop between the 388 instructions of two chunks (9 with 16 waves
+//     and MT = 4, where it has other products to put there; 364 with 12).
 template <int KIND, int SRC, int P, int MT, int NV, int CB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void ss_head_kernel(HeadArgs a) {
   constexpr int THREADS = WAVES * 64;
@@ -686,8 +692,10 @@ static void launch_head_f32(HeadArgs& a, bool direct, int cus, hipStream_t st) {
 //   V = 131072, H = 4096 (32 tiles a compute unit)  16 waves 67 / 88, 14 waves 89, 12 waves 75
 //   V = 98304, H = 4096 (24)                        59 / 76, 58 / 74, 53 / 69
 //   V = 161103, H = 4736 (39.3)                     112 / 136 (mx 153), 107 / 139 (mx 133), 118 / 159 (mx 144)
-// E2M1 has no sums of groups beside the row's, which leaves registers for four tiles of vocabulary rows a wave: T = 64, V = 131072 89
-// against 91 of 16 waves, V = 161103 226 against 133 of 14; T = 320, V = 131072 347 against 381.  Integers spill there (517).
+// E2M1 has no sums of groups beside the row's, so that four tiles of vocabulary rows a wave fit the registers but for 332 bytes a lane that
+// are put aside before and after the loop (none in it): T = 64, V = 131072 89 against 91 of 16 waves, V = 161103 226 against 133 of 14; T =
+// 320, V = 131072 347 against 381.  Integers of groups of 128 and 64 spill in the loop, those of 32 put more aside: T = 320 1095, 960 and 541
+// against 400, 429 and 473 of 16 waves.
 template <int KIND, int MT>
 static void launch_rounds(HeadArgs& a, int64_t work, int cus, hipStream_t st) {
   auto cost = [&](int tiles, int each) { return (work + (int64_t)tiles * cus - 1) / ((int64_t)tiles * cus) * each; };
