@@ -641,13 +641,14 @@ static int compute_units() {
 //   At most one of its workgroups to a compute unit (8 tiles): one round, without a rest.  T = 16: V = 32768, H = 4096 21.3 / 17.4, V = 36869
 //     25.4 / 29.4; where the rows do not fit LDS, a wave takes whole tiles and half of the waves have none: H = 8192, V = 16384 29 / 25, V =
 //     32000 42 / 36, V = 50000 60 / 61; H = 65536, V = 16384 230 / 167.  Long rows that do fit are shared out evenly: H = 8192, V = 16384, T = 8 21.6 / 24.1;
-//     H = 6144, V = 22533, T = 1 21.1 / 22.4, T = 8 23.8 / 23.2; H = 4096, V = 32768, T = 1 17.6 / 16.9.
+//     H = 6144, V = 22533, T = 1 21.1 / 22.4, T = 8 23.8 / 23.2.  So is the time of one row: H = 4096, V = 32768 17.6 / 16.9, and 17.7 /
+//     19.9 at an odd address, whence the other kernel has it copied first (T = 16: 23.7 / 21.1).
 static bool few_pays(const HeadArgs& a, bool f32, int cus) {
   const int64_t tiles = (a.V + 15) / 16, units = (a.nb + kUnit - 1) / kUnit;
   if (tiles * units < (int64_t)2 * kFewWaves * cus) return false;
   if (f32) return true;
   if (a.nb < 4) return false;
-  return tiles > (int64_t)8 * cus || (a.nb >= 48 && units * kUnit * kBlockCols * a.T <= kSlabBytes / 2);
+  return tiles > (int64_t)8 * cus || ((a.nb >= 48 || a.T == 1) && units * kUnit * kBlockCols * a.T <= kSlabBytes / 2);
 }
 
 template <int KIND, int DT>
